@@ -41,6 +41,7 @@
  *   with h in {1, 2, 4, 8}, d <= 256 and m a multiple of 32 up to 128; every other
  *   shape, and all of fp32, runs on the general fp32-arithmetic kernels.
  *   lime_xor_backward: d/h <= 64; its matrix-core form serves bf16 with d/h in {32, 64}, any h and m.
+ *   The history encoder's operators have limits of their own, stated with them.
  */
 #ifndef LIME_H_
 #define LIME_H_
@@ -336,6 +337,87 @@ size_t lime_scores_workspace_bytes(const lime_scoring_model* model, int32_t B, i
 int32_t lime_scores(const lime_scoring_model* model, const void* E, const int32_t* lens, const void* EC, const void* T,
                     void* LC, void* LP, void* O, float* scores, int32_t B, int32_t N, int32_t C, int32_t dtype,
                     void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * A causal encoder of user histories: the operators of its attention block and of its training loss.  The paper encodes users by
+ * L^P alone; the sequence models it is measured against (Section 4.1) let a history's events attend to each other, and are trained
+ * to name the next item.  These are that block's parts, for training (each with its gradients) and serving.  All of them take
+ * LIME_F32 and LIME_BF16, sum in fp32, use no atomics (the same call gives the same bits) and are capturable into a HIP graph.
+ *
+ * lime_norm_rotary - every query and key head normalised and turned by its row's position, in one pass over both:
+ *     n = x / sqrt(mean(x^2) + eps),   z = n * gamma,
+ *     y_i = z_i cos(a_i) - z_{i+dh/2} sin(a_i),   y_{i+dh/2} = z_{i+dh/2} cos(a_i) + z_i sin(a_i),   a_i = position base^(-2 i / dh), i < dh/2.
+ *   Q[rows][hq][dh], K[rows][hk][dh] (hk = 0: no keys, K and KO unused) with q_stride, k_stride elements from row to row: they may be
+ *   columns of one wider projection.  gamma_q, gamma_k [dh], NULL = 1; positions int32 [rows] of any sign (angles are worked out in
+ *   fp64), NULL = no rotation.  QO, KO with strides of their own; they may be Q and K themselves.  dh even, at most 256.
+ * lime_norm_rotary_backward - dQ, dK and (where the pointers are not NULL) dgamma_q, dgamma_k [dh] from dQO, dKO and the forward
+ *   pass's inputs.  dQ may be dQO, dK may be dKO.  Workspace: lime_norm_rotary_backward_workspace_bytes.
+ *
+ * lime_sequence_attention - softmax attention over packed sequences with grouped heads:
+ *     O_i = sum_j softmax_j(scale <Q_i, K_j>) V_j   per query head, on key head (query head) / (hq / hk); hq a multiple of hk.
+ *   Q, O [q_rows][hq][dh], K, V [k_rows][hk][dh]; Q, K and V with strides of their own, O without gaps; dh at most 128.
+ *   `where` (a HOST struct) says which rows belong to whom: user b's slot is rows q_offsets[b] .. q_offsets[b+1] - 1 of Q and
+ *   k_offsets[b] .. k_offsets[b+1] - 1 of K and V (offsets ascending), and the first q_lens[b], k_lens[b] rows of a slot are in use
+ *   (NULL: all).  Packed histories have no lens; a padded batch or a cache with room for N events a user has offsets b * N.
+ *   max_q, max_k: at least the longest slot; what lies past them in a slot is neither read nor written.  Offsets and lengths are
+ *   device memory and are not checked, only cut to the tensors and slots.
+ *   causal: a user's rows count from the end, query i of n_q sees the keys j <= i + n_k - n_q of n_k.  So n_q = n_k is a history on
+ *   its own, n_q = 1 one new event over its history (its own key the last), and n_q between them a few new events at once; where
+ *   n_q > n_k the first queries see nothing.  causal = 0: every query sees all keys of its user.
+ *   A row that sees no key gets zeros.  Rows of a slot not in use are never read and get zeros in O; rows outside all slots are left
+ *   as they were.  Entries that are not finite stay with their user (a key that a query does not see may still turn the rows of
+ *   its user's neighbouring queries to NaN if its value row is not finite).
+ *   lse [q_rows][hq] fp32, nullable: log sum_j exp(scale <Q_i, K_j>), -infinity for rows that see nothing or are not in use.
+ *   Few queries over many keys (serving) have the keys cut into chunks whose states are folded by a second kernel.
+ * lime_sequence_attention_backward - dQ, dK, dV from dO and the forward pass's inputs and outputs O, lse (same sizes, same
+ *   `where`).  dQ, dK, dV have strides of their own (they may be columns of one wider gradient); gradients of a key head are summed
+ *   over its query heads.  Rows of a slot not in use get zeros, rows outside all slots are left as they were.
+ *   Workspace of both: lime_sequence_attention_workspace_bytes.
+ *
+ * lime_catalogue_loss - softmax cross entropy of rows against a catalogue of items, the logits never in memory:
+ *     z_iv = scale <X_i, W_v>,   lse_i = log sum_v exp(z_iv),   loss_i = lse_i - z_{i,targets[i]}.
+ *   X[rows][d], W[n_items][d], d at most 256; targets int32 [rows] on the device: a row whose target is outside [0, n_items) has
+ *   none; it is not read, its loss and lse are 0.  Out: loss, lse [rows], always fp32.
+ * lime_catalogue_loss_backward - from dloss[rows] (fp32) and the forward pass's inputs and lse:
+ *     e_iv = dloss_i scale (exp(z_iv - lse_i) - [v = targets[i]]),   dX_i = sum_v e_iv W_v,   dW_v = sum_i e_iv X_i;
+ *   dX or dW NULL: not wanted.  Rows without a target get zeros and add nothing to dW.
+ *   Workspace of both: lime_catalogue_loss_workspace_bytes.
+ *
+ * Strides are at least a row's own elements and below 2^24 bytes.  Pointers, strides and head rows that are multiples of 16 bytes
+ * are read 16 bytes a lane, anything else element by element (slower; sums may be in another order).  Workspaces are 256-byte aligned.
+ */
+typedef struct lime_sequences {
+  const int32_t *q_offsets, *k_offsets; /* [B + 1] */
+  const int32_t *q_lens, *k_lens;       /* [B], nullable */
+  int64_t q_rows, k_rows;               /* rows of Q, and of K and V; may be 0 */
+  int32_t B, max_q, max_k;
+} lime_sequences;
+
+int32_t lime_norm_rotary(const void* Q, int64_t q_stride, const void* K, int64_t k_stride, const void* gamma_q, const void* gamma_k,
+                         const int32_t* positions, float base, float eps, void* QO, int64_t qo_stride, void* KO, int64_t ko_stride,
+                         int64_t rows, int32_t hq, int32_t hk, int32_t dh, int32_t dtype, void* stream);
+size_t lime_norm_rotary_backward_workspace_bytes(int64_t rows, int32_t dh);
+int32_t lime_norm_rotary_backward(const void* dQO, int64_t dqo_stride, const void* dKO, int64_t dko_stride, const void* Q, int64_t q_stride,
+                                  const void* K, int64_t k_stride, const void* gamma_q, const void* gamma_k, const int32_t* positions,
+                                  float base, float eps, void* dQ, int64_t dq_stride, void* dK, int64_t dk_stride, void* dgamma_q,
+                                  void* dgamma_k, int64_t rows, int32_t hq, int32_t hk, int32_t dh, int32_t dtype, void* workspace,
+                                  size_t ws_bytes, void* stream);
+size_t lime_sequence_attention_workspace_bytes(const lime_sequences* where, int32_t hq, int32_t hk, int32_t dh, int32_t dtype,
+                                               int32_t backward);
+int32_t lime_sequence_attention(const lime_sequences* where, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
+                                const void* V, int64_t v_stride, void* O, float* lse, int32_t hq, int32_t hk, int32_t dh, float scale,
+                                int32_t causal, int32_t dtype, void* workspace, size_t ws_bytes, void* stream);
+int32_t lime_sequence_attention_backward(const lime_sequences* where, const void* dO, const void* Q, int64_t q_stride, const void* K,
+                                         int64_t k_stride, const void* V, int64_t v_stride, const void* O, const float* lse, void* dQ,
+                                         int64_t dq_stride, void* dK, int64_t dk_stride, void* dV, int64_t dv_stride, int32_t hq,
+                                         int32_t hk, int32_t dh, float scale, int32_t causal, int32_t dtype, void* workspace,
+                                         size_t ws_bytes, void* stream);
+size_t lime_catalogue_loss_workspace_bytes(int64_t rows, int32_t n_items, int32_t d, int32_t dtype, int32_t backward);
+int32_t lime_catalogue_loss(const void* X, const void* W, const int32_t* targets, float* loss, float* lse, int64_t rows, int32_t n_items,
+                            int32_t d, float scale, int32_t dtype, void* workspace, size_t ws_bytes, void* stream);
+int32_t lime_catalogue_loss_backward(const float* dloss, const void* X, const void* W, const int32_t* targets, const float* lse, void* dX,
+                                     void* dW, int64_t rows, int32_t n_items, int32_t d, float scale, int32_t dtype, void* workspace,
+                                     size_t ws_bytes, void* stream);
 
 /*
  * Workspace size in bytes for `op` (LIME_OP_*) at the given shape; dimensions an op

@@ -92,6 +92,30 @@ SIGNATURES.update({
     "lime_scores": (_i32, [_c.POINTER(ScoringModel), _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _sz, _vp]),
 })
 
+
+
+class Sequences(_c.Structure):
+    """lime_sequences of include/lime.h (a host struct): which packed rows belong to whom."""
+    _fields_ = [("q_offsets", _vp), ("k_offsets", _vp), ("q_lens", _vp), ("k_lens", _vp), ("q_rows", _i64), ("k_rows", _i64),
+                ("B", _i32), ("max_q", _i32), ("max_k", _i32)]
+
+
+_seq = _c.POINTER(Sequences)
+SIGNATURES.update({
+    "lime_norm_rotary": (_i32, [_vp, _i64, _vp, _i64, _vp, _vp, _vp, _f32, _f32, _vp, _i64, _vp, _i64, _i64, _i32, _i32, _i32, _i32,
+                                _vp]),
+    "lime_norm_rotary_backward_workspace_bytes": (_sz, [_i64, _i32]),
+    "lime_norm_rotary_backward": (_i32, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _f32, _f32, _vp, _i64, _vp, _i64, _vp,
+                                         _vp, _i64, _i32, _i32, _i32, _i32, _vp, _sz, _vp]),
+    "lime_sequence_attention_workspace_bytes": (_sz, [_seq, _i32, _i32, _i32, _i32, _i32]),
+    "lime_sequence_attention": (_i32, [_seq, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i32, _i32, _i32, _f32, _i32, _i32, _vp, _sz, _vp]),
+    "lime_sequence_attention_backward": (_i32, [_seq, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _i32,
+                                                _i32, _i32, _f32, _i32, _i32, _vp, _sz, _vp]),
+    "lime_catalogue_loss_workspace_bytes": (_sz, [_i64, _i32, _i32, _i32, _i32]),
+    "lime_catalogue_loss": (_i32, [_vp] * 5 + [_i64, _i32, _i32, _f32, _i32, _vp, _sz, _vp]),
+    "lime_catalogue_loss_backward": (_i32, [_vp] * 7 + [_i64, _i32, _i32, _f32, _i32, _vp, _sz, _vp]),
+})
+
 _lib = None
 _native_module = None
 
@@ -453,3 +477,46 @@ def lime_scores(model: ScoringModel, E, lens, EC, T, want_intermediates=False, w
     """One LIME-MHA request from embeddings to scores (Eq. 2 -> LN -> Eq. 3 -> LN -> Eq. 4 -> interaction network).
     Returns scores [B, C] (fp32), and with want_intermediates also (LC, LP, O)."""
     return _native().scores(model, E, lens, EC, T, want_intermediates, workspace, stream)
+
+
+# ------------------------------------------------------------------------------------------------- a causal encoder of histories
+# The tensors of these calls are [rows, heads, dh] with rows a stride of their own apart (columns of a wider projection).  Outputs
+# that are not given are allocated on the call's stream.  Without a workspace, and while the stream is captured into a graph, a call
+# takes a workspace of its own from the graph's memory; otherwise get_workspace's.
+def lime_norm_rotary(Q, K, gamma_q=None, gamma_k=None, positions=None, base=10000.0, eps=1e-6, QO=None, KO=None, stream=None):
+    """(QO, KO): every head of Q[rows, hq, dh] and K[rows, hk, dh] (or None) over its root mean square, times gamma [dh], its pairs
+    (i, i + dh/2) turned by positions[row] * base^(-2i/dh) (positions int32 [rows], None = not turned).  QO, KO may be Q, K."""
+    return _native().norm_rotary(Q, K, gamma_q, gamma_k, positions, base, eps, QO, KO, stream)
+
+
+def lime_norm_rotary_backward(dQO, dKO, Q, K, gamma_q=None, gamma_k=None, positions=None, base=10000.0, eps=1e-6, dQ=None, dK=None,
+                              workspace=None, stream=None):
+    """(dQ, dK, dgamma_q, dgamma_k) of lime_norm_rotary; the gradient of a gamma that is None is None."""
+    return _native().norm_rotary_backward(dQO, dKO, Q, K, gamma_q, gamma_k, positions, base, eps, dQ, dK, workspace, stream)
+
+
+def lime_sequence_attention(Q, K, V, q_offsets, k_offsets, max_q, max_k, scale, q_lens=None, k_lens=None, causal=True, O=None, lse=None,
+                            workspace=None, stream=None):
+    """(O[q_rows, hq, dh], lse[q_rows, hq] fp32): softmax attention of each user's queries over that user's keys, K and V
+    [k_rows, hk, dh].  User b has rows q_offsets[b] .. q_offsets[b+1] of Q, of which the first q_lens[b] are in use (None: all),
+    and likewise of K and V; max_q, max_k: at least the longest slot.  causal: rows are aligned at their ends, so one new event
+    over its history is a single query.  Offsets and lengths are int32 on the device."""
+    return _native().sequence_attention(Q, K, V, q_offsets, k_offsets, max_q, max_k, scale, q_lens, k_lens, causal, O, lse, workspace, stream)
+
+
+def lime_sequence_attention_backward(dO, Q, K, V, O, lse, q_offsets, k_offsets, max_q, max_k, scale, q_lens=None, k_lens=None, causal=True,
+                                     dQ=None, dK=None, dV=None, workspace=None, stream=None):
+    """(dQ, dK, dV) of lime_sequence_attention from its inputs and outputs."""
+    return _native().sequence_attention_backward(dO, Q, K, V, O, lse, q_offsets, k_offsets, max_q, max_k, scale, q_lens, k_lens, causal, dQ, dK,
+                                                 dV, workspace, stream)
+
+
+def lime_catalogue_loss(X, W, targets, scale=1.0, loss=None, lse=None, workspace=None, stream=None):
+    """(loss[rows], lse[rows]), fp32: softmax cross entropy of X[rows, d] against the items W[n_items, d], logits scale <X_i, W_v>;
+    targets int32 [rows], a target outside [0, n_items): the row has none (loss and lse 0, nothing read)."""
+    return _native().catalogue_loss(X, W, targets, scale, loss, lse, workspace, stream)
+
+
+def lime_catalogue_loss_backward(dloss, X, W, targets, lse, scale=1.0, dX=None, dW=None, workspace=None, stream=None):
+    """(dX[rows, d], dW[n_items, d]) of lime_catalogue_loss for dloss[rows] (fp32)."""
+    return _native().catalogue_loss_backward(dloss, X, W, targets, lse, scale, dX, dW, workspace, stream)

@@ -1,0 +1,497 @@
+// Softmax cross entropy of rows over a catalogue of items, with its gradients, the logits never in memory:
+//   z_iv = scale <X_i, W_v>,   lse_i = log sum_v exp(z_iv),   loss_i = lse_i - z_i,target(i)
+//   e_iv = dloss_i scale (exp(z_iv - lse_i) - [v = target(i)]),   dX_i = sum_v e_iv W_v,   dW_v = sum_i e_iv X_i.
+// Rows without a target have no loss and no gradients, and nothing of them is read into any: the other rows are listed first and,
+// where there are any to leave out, copied together (gather), so that padding costs no products.
+// The forward pass and dX hold rows of X in registers and stream the items' tiles, with the catalogue cut into chunks whose sums
+// are folded in ascending order; dW holds items and streams rows.  The target's own term of dX is added in fp32 at the fold.
+#include <algorithm>
+
+#include "encoder.hpp"
+#include "tiles.hpp"
+
+namespace lime {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct Args {
+  const void *x, *w;
+  const int32_t* targets;
+  float *loss, *lse;
+  const float* dloss;
+  void *dx, *dw;
+  int64_t rows;
+  int items, d;
+  float scale;
+  bool x_pieces, w_pieces, quads;
+  // workspace
+  int32_t* live;      // [1 + rows]: how many rows have a target, and which they are
+  void* packed;       // [rows][d] the rows with a target, written where some have none
+  float *c_lse2, *c_g;  // [rows] of the listed rows: lse log2 e; dloss scale
+  int32_t* c_target;  // [rows]
+  float* parts;       // forward [splits][rows][2], dX [splits][rows][padded d], dW [splits][items][padded d]
+  int splits, chunk;
+};
+
+constexpr int kGatherRows = 64;  // the fewest rows a workgroup of the gather takes
+
+// Lists the rows with a target.  Every workgroup counts all targets by itself (they are few next to the products), so that no
+// workgroup waits for another.
+template <typename T, bool BACKWARD>
+__global__ __launch_bounds__(256) void gather_kernel(Args a, int64_t each) {
+  __shared__ int sums[4][2];
+  __shared__ int place[256];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t begin = blockIdx.x * each, end = min(begin + each, a.rows);
+  auto has = [&](int64_t i) { return static_cast<unsigned>(a.targets[i]) < static_cast<unsigned>(a.items); };
+  int before = 0, all = 0;
+  for (int64_t i = tid; i < a.rows; i += 256) {
+    const int x = has(i);
+    all += x, before += i < begin ? x : 0;
+  }
+  for (int o = 32; o; o >>= 1) before += __shfl_xor(before, o, 64), all += __shfl_xor(all, o, 64);
+  if (lane == 0) sums[wave][0] = before, sums[wave][1] = all;
+  __syncthreads();
+  before = sums[0][0] + sums[1][0] + sums[2][0] + sums[3][0], all = sums[0][1] + sums[1][1] + sums[2][1] + sums[3][1];
+  if (blockIdx.x == 0 && tid == 0) a.live[0] = all;
+  const bool whole = all == a.rows;
+  for (int64_t at = begin; at < end; at += 256) {
+    const int64_t i = at + tid;
+    const bool x = i < end && has(i);
+    const unsigned long long votes = __ballot(x);
+    __syncthreads();
+    if (lane == 0) sums[wave][0] = __popcll(votes);
+    __syncthreads();
+    int to = before + __popcll(votes & ((1ull << lane) - 1));
+    for (int w = 0; w < wave; ++w) to += sums[w][0];
+    before += sums[0][0] + sums[1][0] + sums[2][0] + sums[3][0];
+    place[tid] = x ? to : -1;
+    if (x) {
+      a.live[1 + to] = static_cast<int>(i);
+      if constexpr (BACKWARD) a.c_lse2[to] = a.lse[i] * kLog2e, a.c_g[to] = a.dloss[i] * a.scale, a.c_target[to] = a.targets[i];
+    } else if (i < end) {
+      if constexpr (!BACKWARD) a.loss[i] = 0.f, a.lse[i] = 0.f;
+    }
+    if (whole) continue;
+    __syncthreads();
+    const int64_t here = min<int64_t>(256, end - at) * a.d;
+    for (int64_t e = tid; e < here; e += 256) {
+      const int r = static_cast<int>(e / a.d), c = static_cast<int>(e % a.d);
+      if (place[r] >= 0) static_cast<T*>(a.packed)[static_cast<int64_t>(place[r]) * a.d + c] = static_cast<const T*>(a.x)[(at + r) * a.d + c];
+      else if (BACKWARD && a.dx) store_as(static_cast<T*>(a.dx) + (at + r) * a.d + c, 0.f);
+    }
+  }
+}
+
+// The listed rows of X: X itself where every row is listed.
+template <typename T>
+__device__ __forceinline__ const T* listed_rows(const Args& a, int count) {
+  return static_cast<const T*>(count == a.rows ? a.x : a.packed);
+}
+
+// Running maximum and sum of a chunk of the catalogue for 32 rows a wave (as in the attention's forward pass, see there).
+constexpr float kHeadroom = 8.f;
+template <typename T, int D, int STEP>
+__global__ __launch_bounds__(256) void catalogue_lse_kernel(Args a) {
+  using Shape = Tile<T, D, STEP>;
+  using Loader = TileLoader<T, D, STEP, 4>;
+  constexpr int VB = STEP / 32, NK = D / 16;
+  extern __shared__ __align__(1024) unsigned char smem[];  // [2] tiles
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
+  const int split = blockIdx.x % a.splits, tile = blockIdx.x / a.splits, count = a.live[0];
+  if (tile * 128 >= count) return;
+  const int row = tile * 128 + 32 * wave + n;
+  const int v0 = split * a.chunk, v1 = min(a.items, v0 + a.chunk), steps = (v1 - v0 + STEP - 1) / STEP;
+  const unsigned width = a.d * sizeof(T);
+  const Rows wm{static_cast<const T*>(a.w) + static_cast<int64_t>(v0) * a.d, width, width, a.w_pieces};
+  Loader wl;
+  wl.init(wm, tid);
+  wl.issue(wm, 0, v1 - v0, smem, tid);
+  Fragment<T> x[NK];
+  load_row<T, D>(listed_rows<T>(a, count) + static_cast<int64_t>(row) * a.d, width, a.x_pieces, row < count, g, x);
+  const float c = fmaxf(fabsf(a.scale) * kLog2e, 1e-37f);
+  if (a.scale < 0.f) {
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) x[kk] = -x[kk];
+  }
+  float m = -INFINITY, l = 0.f;
+  for (int i = 0; i < steps; ++i) {
+    wait_lds_loads<0>();
+    lds_barrier();
+    if (i + 1 < steps) wl.issue(wm, (i + 1) * STEP, v1 - v0, smem + (i + 1) % 2 * Shape::kBytes, tid);
+    const unsigned char* wt = smem + i % 2 * Shape::kBytes;
+    f32x16 s[VB];
+#pragma unroll
+    for (int vb = 0; vb < VB; ++vb) {
+      s[vb] = zero_block();
+#pragma unroll
+      for (int kk = 0; kk < NK; ++kk) s[vb] = mma16(Shape::row_fragment(wt, 32 * vb, kk, lane), x[kk], s[vb]);
+    }
+    if (v0 + (i + 1) * STEP > v1) {
+#pragma unroll
+      for (int vb = 0; vb < VB; ++vb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (v0 + i * STEP + 32 * vb + block_row(e, g) >= v1) s[vb][e] = -INFINITY;
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int vb = 0; vb < VB; ++vb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[vb][e]);
+    top = pair_max(top) * c;
+    if (__any(top > m + kHeadroom)) {
+      const float to = fmaxf(m, top);
+      l *= to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
+      m = to;
+    }
+    const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int vb = 0; vb < VB; ++vb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) l += __builtin_amdgcn_exp2f(fmaf(s[vb][e], c, -base));
+  }
+  l = pair_sum(l);
+  if (row < count && g == 0) {
+    float* to = a.parts + (static_cast<int64_t>(split) * a.rows + row) * 2;
+    to[0] = m, to[1] = l;
+  }
+}
+
+// A wave a row: the chunks' states folded, and the target's logit.
+template <typename T>
+__global__ __launch_bounds__(256) void catalogue_loss_kernel(Args a) {
+  const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6), count = a.live[0];
+  if (row >= count) return;
+  const int at = a.live[1 + row], target = a.targets[at];
+  float m = -INFINITY, l = 0.f;
+  for (int s = lane; s < a.splits; s += 64) {
+    const float* p = a.parts + (static_cast<int64_t>(s) * a.rows + row) * 2;
+    const float to = fmaxf(m, p[0]), base = to == -INFINITY ? 0.f : to;
+    l = l * __builtin_amdgcn_exp2f(m - base) + p[1] * __builtin_amdgcn_exp2f(p[0] - base);
+    m = to;
+  }
+  float most = m;
+  for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
+  const float base = most == -INFINITY ? 0.f : most;
+  const float sum = wave_sum(l * __builtin_amdgcn_exp2f(m - base));
+  const T *x = static_cast<const T*>(a.x) + static_cast<int64_t>(at) * a.d, *w = static_cast<const T*>(a.w) + static_cast<int64_t>(target) * a.d;
+  float z = 0.f;
+  for (int c = lane; c < a.d; c += 64) z = fmaf(to_float(x[c]), to_float(w[c]), z);
+  z = wave_sum(z) * a.scale;
+  if (lane == 0) {
+    const float lse = (most + __builtin_amdgcn_logf(sum)) * kLn2;
+    a.lse[at] = lse, a.loss[at] = lse - z;
+  }
+}
+
+// sum_v p_iv W_v over a chunk of the catalogue, 32 rows a wave.
+template <typename T, int D, int STEP>
+__global__ __launch_bounds__(256) void catalogue_dx_kernel(Args a) {
+  using Shape = Tile<T, D, STEP>;
+  using Loader = TileLoader<T, D, STEP, 4>;
+  constexpr int VB = STEP / 32, NK = D / 16, OB = D / 32;
+  extern __shared__ __align__(1024) unsigned char smem[];  // [2] tiles
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
+  const int split = blockIdx.x % a.splits, tile = blockIdx.x / a.splits, count = a.live[0];
+  if (tile * 128 >= count) return;
+  const int row = tile * 128 + 32 * wave + n;
+  const int v0 = split * a.chunk, v1 = min(a.items, v0 + a.chunk), steps = (v1 - v0 + STEP - 1) / STEP;
+  const unsigned width = a.d * sizeof(T);
+  const Rows wm{static_cast<const T*>(a.w) + static_cast<int64_t>(v0) * a.d, width, width, a.w_pieces};
+  Loader wl;
+  wl.init(wm, tid);
+  wl.issue(wm, 0, v1 - v0, smem, tid);
+  Fragment<T> x[NK];
+  load_row<T, D>(listed_rows<T>(a, count) + static_cast<int64_t>(row) * a.d, width, a.x_pieces, row < count, g, x);
+  const float c = a.scale * kLog2e, lse2 = row < count ? a.c_lse2[row] : 0.f;
+  f32x16 dx[OB];
+#pragma unroll
+  for (int ob = 0; ob < OB; ++ob) dx[ob] = zero_block();
+  for (int i = 0; i < steps; ++i) {
+    wait_lds_loads<0>();
+    lds_barrier();
+    if (i + 1 < steps) wl.issue(wm, (i + 1) * STEP, v1 - v0, smem + (i + 1) % 2 * Shape::kBytes, tid);
+    const unsigned char* wt = smem + i % 2 * Shape::kBytes;
+#pragma unroll
+    for (int vb = 0; vb < VB; ++vb) {
+      f32x16 p = zero_block();
+#pragma unroll
+      for (int kk = 0; kk < NK; ++kk) p = mma16(Shape::row_fragment(wt, 32 * vb, kk, lane), x[kk], p);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(p[e], c, -lse2));
+      if (v0 + (i + 1) * STEP > v1) {  // (zero rows past the chunk: p may be infinite there)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (v0 + i * STEP + 32 * vb + block_row(e, g) >= v1) p[e] = 0.f;
+      }
+#pragma unroll
+      for (int f = 0; f < 2; ++f) {
+        const Fragment<T> pf = half_fragment<T>(p, f);
+#pragma unroll
+        for (int ob = 0; ob < OB; ++ob) dx[ob] = mma16(Shape::column_fragment(wt, 32 * vb + 16 * f, 32 * ob, lane), pf, dx[ob]);
+      }
+    }
+  }
+  if (row >= count) return;
+  float* to = a.parts + (static_cast<int64_t>(split) * a.rows + row) * D;
+#pragma unroll
+  for (int ob = 0; ob < OB; ++ob) store_block(to, dx[ob], 1.f, 32 * ob, D, true, g);
+}
+
+// dX_i = dloss_i scale (the chunks' sums - W_target), D / 4 lanes a row.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void catalogue_dx_fold_kernel(Args a) {
+  constexpr int LANES = D / 4;
+  const int row = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, c = threadIdx.x % LANES * 4, count = a.live[0];
+  if (row >= count || c >= a.d) return;
+  f32x4 sum = {0, 0, 0, 0};
+  for (int s = 0; s < a.splits; ++s) {
+    const f32x4 p = *reinterpret_cast<const f32x4*>(a.parts + (static_cast<int64_t>(s) * a.rows + row) * D + c);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum[j] += p[j];
+  }
+  const T* w = static_cast<const T*>(a.w) + static_cast<int64_t>(a.c_target[row]) * a.d + c;
+  T* to = static_cast<T*>(a.dx) + static_cast<int64_t>(a.live[1 + row]) * a.d + c;
+  const float f = a.c_g[row];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (c + j < a.d) store_as(to + j, f * (sum[j] - to_float(w[j])));
+}
+
+// sum_i e_iv X_i over a chunk of the listed rows, 32 items a wave.
+template <typename T, int D, int STEP>
+__global__ __launch_bounds__(256) void catalogue_dw_kernel(Args a) {
+  using Shape = Tile<T, D, STEP>;
+  using Loader = TileLoader<T, D, STEP, 4>;
+  constexpr int RB = STEP / 32, NK = D / 16, OB = D / 32, kStage = Shape::kBytes + 1024;  // rows; lse2, dloss scale, target, each [64]
+  extern __shared__ __align__(1024) unsigned char smem[];                                 // [2] stages
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
+  const int split = blockIdx.x % a.splits, tile = blockIdx.x / a.splits, count = a.live[0];
+  const int item0 = tile * 128 + 32 * wave, item = item0 + n;
+  const int i0 = split * a.chunk, i1 = min(count, i0 + a.chunk), steps = i1 > i0 ? (i1 - i0 + STEP - 1) / STEP : 0;
+  const unsigned width = a.d * sizeof(T);
+  const Rows xm{listed_rows<T>(a, count) + static_cast<int64_t>(i0) * a.d, width, width, a.x_pieces};
+  Loader xl;
+  xl.init(xm, tid);
+  auto ask = [&](int i) {
+    unsigned char* at = smem + i % 2 * kStage;
+    xl.issue(xm, i * STEP, i1 - i0, at, tid);
+    const int from = i0 + i * STEP;
+    const void* words = wave == 0 ? static_cast<const void*>(a.c_lse2 + from) : wave == 1 ? static_cast<const void*>(a.c_g + from) : static_cast<const void*>(a.c_target + from);
+    if (wave < 3) words_to_lds(words, min(STEP, i1 - from), at + Shape::kBytes + 256 * wave, lane);
+  };
+  if (steps > 0) ask(0);
+  Fragment<T> w[NK];
+  load_row<T, D>(static_cast<const T*>(a.w) + static_cast<int64_t>(item) * a.d, width, a.w_pieces, item < a.items, g, w);
+  const float c = a.scale * kLog2e;
+  f32x16 dw[OB];
+#pragma unroll
+  for (int ob = 0; ob < OB; ++ob) dw[ob] = zero_block();
+  for (int i = 0; i < steps; ++i) {
+    wait_lds_loads<0>();
+    lds_barrier();
+    if (i + 1 < steps) ask(i + 1);
+    const unsigned char* xt = smem + i % 2 * kStage;
+    const float *lse2 = reinterpret_cast<const float*>(xt + Shape::kBytes), *weight = lse2 + 64;
+    const int32_t* target = reinterpret_cast<const int32_t*>(weight + 64);
+    // whether any of the step's rows has one of the wave's items for its target (rows past the last have the weight 0)
+    const bool chosen = __any(static_cast<unsigned>(target[lane % STEP] - item0) < 32u);
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      f32x16 e = zero_block();
+#pragma unroll
+      for (int kk = 0; kk < NK; ++kk) e = mma16(Shape::row_fragment(xt, 32 * rb, kk, lane), w[kk], e);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int at = 32 * rb + 8 * j + 4 * g;
+        const f32x4 l4 = *reinterpret_cast<const f32x4*>(lse2 + at);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) e[4 * j + y] = __builtin_amdgcn_exp2f(fmaf(e[4 * j + y], c, -l4[y]));
+        if (chosen) {
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+            if (target[at + y] == item) e[4 * j + y] -= 1.f;
+        }
+        const f32x4 g4 = *reinterpret_cast<const f32x4*>(weight + at);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) e[4 * j + y] *= g4[y];
+      }
+#pragma unroll
+      for (int f = 0; f < 2; ++f) {
+        const Fragment<T> ef = half_fragment<T>(e, f);
+#pragma unroll
+        for (int ob = 0; ob < OB; ++ob) dw[ob] = mma16(Shape::column_fragment(xt, 32 * rb + 16 * f, 32 * ob, lane), ef, dw[ob]);
+        // A target's e is near its row's whole weight and rarely has company: what rounding took of it is added by itself.
+        if (sizeof(T) == 2 && chosen) {
+          Fragment<T> rest;
+#pragma unroll
+          for (int t = 0; t < 8; ++t) {
+            const float x = e[8 * f + t];
+            rest[t] = static_cast<std::conditional_t<sizeof(T) == 2, __bf16, float>>(target[32 * rb + block_row(8 * f + t, g)] == item ? x - static_cast<float>(ef[t]) : 0.f);
+          }
+#pragma unroll
+          for (int ob = 0; ob < OB; ++ob) dw[ob] = mma16(Shape::column_fragment(xt, 32 * rb + 16 * f, 32 * ob, lane), rest, dw[ob]);
+        }
+      }
+    }
+  }
+  if (item >= a.items) return;
+  if (a.splits > 1) {
+    float* to = a.parts + (static_cast<int64_t>(split) * a.items + item) * D;
+#pragma unroll
+    for (int ob = 0; ob < OB; ++ob) store_block(to, dw[ob], 1.f, 32 * ob, D, true, g);
+  } else {
+    T* to = static_cast<T*>(a.dw) + static_cast<int64_t>(item) * a.d;
+#pragma unroll
+    for (int ob = 0; ob < OB; ++ob) store_block(to, dw[ob], 1.f, 32 * ob, a.d, a.quads, g);
+  }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void catalogue_dw_fold_kernel(Args a) {
+  constexpr int LANES = D / 4;
+  const int64_t item = static_cast<int64_t>(blockIdx.x) * (256 / LANES) + threadIdx.x / LANES;
+  const int c = threadIdx.x % LANES * 4;
+  if (item >= a.items || c >= a.d) return;
+  f32x4 sum = {0, 0, 0, 0};
+  for (int s = 0; s < a.splits; ++s) {
+    const f32x4 p = *reinterpret_cast<const f32x4*>(a.parts + (static_cast<int64_t>(s) * a.items + item) * D + c);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum[j] += p[j];
+  }
+  T* to = static_cast<T*>(a.dw) + item * a.d + c;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (c + j < a.d) store_as(to + j, sum[j]);
+}
+
+int padded(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
+
+// The streamed side cut into chunks so that the workgroups fill the chip: `tiles` of the side that stays, `length` of the other.
+struct Cut {
+  int splits, chunk;
+};
+Cut cut(int64_t tiles, int64_t length, int step, int64_t want) {
+  int64_t splits = tiles >= want ? 1 : (want + tiles - 1) / tiles;
+  splits = std::max<int64_t>(1, std::min(splits, (length + step - 1) / step));
+  int64_t chunk = (length + splits - 1) / splits;
+  chunk = (chunk + step - 1) / step * step;
+  return {static_cast<int>((length + chunk - 1) / chunk), static_cast<int>(chunk)};
+}
+
+struct Plan {
+  Cut rows, items;  // of the kernels that hold rows (chunks of items), that hold items (chunks of rows)
+  size_t live, packed, listed, parts, bytes;
+};
+Plan plan_of(int64_t rows, int items, int d, int dtype, bool backward) {
+  Plan p{};
+  const int step = dtype == 1 ? 64 : 32, D = padded(d);
+  const int64_t want = 2 * static_cast<int64_t>(compute_units());
+  p.rows = cut((rows + 127) / 128, items, step, want);
+  p.items = cut((static_cast<int64_t>(items) + 127) / 128, rows, step, want);
+  p.live = align_up((rows + 1) * sizeof(int32_t));
+  p.packed = align_up(static_cast<size_t>(rows) * d * (dtype == 1 ? 2 : 4));
+  p.listed = backward ? align_up(rows * sizeof(float)) : 0;
+  const size_t by_rows = static_cast<size_t>(p.rows.splits) * rows * (backward ? D : 2) * sizeof(float);
+  const size_t by_items = backward && p.items.splits > 1 ? static_cast<size_t>(p.items.splits) * items * D * sizeof(float) : 0;
+  p.parts = align_up(std::max(by_rows, by_items));
+  p.bytes = p.live + p.packed + 3 * p.listed + p.parts;
+  return p;
+}
+
+bool multiple(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+Args args_of(const CatalogueLoss& x, const Plan& p, void* workspace) {
+  const size_t e = x.dtype == 1 ? 2 : 4;
+  Args a{};
+  a.x = x.X, a.w = x.W, a.targets = x.targets, a.loss = x.loss, a.lse = x.lse, a.dloss = x.dloss, a.dx = x.dX, a.dw = x.dW;
+  a.rows = x.rows, a.items = x.items, a.d = x.d, a.scale = x.scale;
+  a.x_pieces = multiple(x.X, 16) && x.d * e % 16 == 0, a.w_pieces = multiple(x.W, 16) && x.d * e % 16 == 0;
+  a.quads = x.d % 4 == 0 && multiple(x.dW, 4 * e);
+  char* at = static_cast<char*>(workspace);
+  a.live = reinterpret_cast<int32_t*>(at), at += p.live;
+  a.packed = at, at += p.packed;
+  a.c_lse2 = reinterpret_cast<float*>(at), at += p.listed;
+  a.c_g = reinterpret_cast<float*>(at), at += p.listed;
+  a.c_target = reinterpret_cast<int32_t*>(at), at += p.listed;
+  a.parts = reinterpret_cast<float*>(at);
+  return a;
+}
+
+template <typename T, bool BACKWARD>
+hipError_t gather(const Args& a, hipStream_t s) {
+  const int64_t each = std::max<int64_t>(kGatherRows, (a.rows + 255) / 256);
+  hipLaunchKernelGGL((gather_kernel<T, BACKWARD>), dim3(static_cast<unsigned>((a.rows + each - 1) / each)), dim3(256), 0, s, a, each);
+  return hipGetLastError();
+}
+
+template <typename K>
+hipError_t launch(PerDevice& granted, K kernel, int64_t blocks, int lds, const Args& a, hipStream_t s) {
+  if (hipError_t e = allow_lds(granted, reinterpret_cast<const void*>(kernel), lds); e != hipSuccess) return e;
+  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), lds, s, a);
+  return hipGetLastError();
+}
+
+template <typename T, int D>
+hipError_t forward(Args a, const Plan& p, hipStream_t s) {
+  constexpr int STEP = sizeof(T) == 2 ? 64 : 32;
+  if (hipError_t e = gather<T, false>(a, s); e != hipSuccess) return e;
+  static PerDevice granted;
+  a.splits = p.rows.splits, a.chunk = p.rows.chunk;
+  if (hipError_t e = launch(granted, catalogue_lse_kernel<T, D, STEP>, (a.rows + 127) / 128 * a.splits, 2 * Tile<T, D, STEP>::kBytes, a, s); e != hipSuccess) return e;
+  hipLaunchKernelGGL(catalogue_loss_kernel<T>, dim3(static_cast<unsigned>((a.rows + 3) / 4)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+template <typename T, int D>
+hipError_t backward(Args a, const Plan& p, hipStream_t s) {
+  constexpr int STEP = sizeof(T) == 2 ? 64 : 32, PER = 256 / (D / 4);
+  if (hipError_t e = gather<T, true>(a, s); e != hipSuccess) return e;
+  if (a.dx) {
+    static PerDevice granted;
+    a.splits = p.rows.splits, a.chunk = p.rows.chunk;
+    if (hipError_t e = launch(granted, catalogue_dx_kernel<T, D, STEP>, (a.rows + 127) / 128 * a.splits, 2 * Tile<T, D, STEP>::kBytes, a, s); e != hipSuccess) return e;
+    hipLaunchKernelGGL((catalogue_dx_fold_kernel<T, D>), dim3(static_cast<unsigned>((a.rows + PER - 1) / PER)), dim3(256), 0, s, a);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  if (a.dw) {
+    static PerDevice granted;
+    a.splits = p.items.splits, a.chunk = p.items.chunk;
+    const int64_t tiles = (static_cast<int64_t>(a.items) + 127) / 128;
+    if (hipError_t e = launch(granted, catalogue_dw_kernel<T, D, STEP>, tiles * a.splits, 2 * (Tile<T, D, STEP>::kBytes + 1024), a, s); e != hipSuccess) return e;
+    if (a.splits > 1) {
+      hipLaunchKernelGGL((catalogue_dw_fold_kernel<T, D>), dim3(static_cast<unsigned>((static_cast<int64_t>(a.items) + PER - 1) / PER)), dim3(256), 0, s, a);
+      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+
+bool catalogue_loss_fits(int64_t rows, int items) {  // 2^32 work items a launch
+  const int64_t tiles = std::max((rows + 127) / 128, (static_cast<int64_t>(items) + 127) / 128);
+  return rows < (int64_t{1} << 26) - 128 && items <= (1 << 30) && (tiles + 2 * compute_units()) * 256 < (int64_t{1} << 32);
+}
+
+size_t catalogue_loss_workspace(int64_t rows, int items, int d, int dtype, bool backward) { return plan_of(rows, items, d, dtype, backward).bytes; }
+
+hipError_t catalogue_loss(const CatalogueLoss& x, void* workspace, hipStream_t s) {
+  const Plan p = plan_of(x.rows, x.items, x.d, x.dtype, false);
+  const Args a = args_of(x, p, workspace);
+  const int D = padded(x.d);
+  if (x.dtype == 1) return D == 64 ? forward<bf16_t, 64>(a, p, s) : D == 128 ? forward<bf16_t, 128>(a, p, s) : forward<bf16_t, 256>(a, p, s);
+  return D == 64 ? forward<float, 64>(a, p, s) : D == 128 ? forward<float, 128>(a, p, s) : forward<float, 256>(a, p, s);
+}
+
+hipError_t catalogue_loss_backward(const CatalogueLoss& x, void* workspace, hipStream_t s) {
+  const Plan p = plan_of(x.rows, x.items, x.d, x.dtype, true);
+  const Args a = args_of(x, p, workspace);
+  const int D = padded(x.d);
+  if (x.dtype == 1) return D == 64 ? backward<bf16_t, 64>(a, p, s) : D == 128 ? backward<bf16_t, 128>(a, p, s) : backward<bf16_t, 256>(a, p, s);
+  return D == 64 ? backward<float, 64>(a, p, s) : D == 128 ? backward<float, 128>(a, p, s) : backward<float, 256>(a, p, s);
+}
+
+}  // namespace lime

@@ -13,6 +13,7 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/hip/HIPGraphsC10Utils.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -461,6 +462,258 @@ PyObject* scores(Args a) {
   return t;
 }
 
+// ------------------------------------------------------------------------------------------------- the history encoder's calls
+// Device guard and stream of a call whose outputs are allocated within it: they and, under capture, the workspace come from the
+// memory of the call's own stream.
+class OnStream {
+ public:
+  OnStream(const Tensor& like, PyObject* stream)
+      : guard_(like.device()), device_(like.device()), before_(c10::hip::getCurrentHIPStream(device_.index())),
+        stream_(stream_handle(stream, device_.index())), other_(stream_ != before_.stream()) {
+    if (other_) c10::hip::setCurrentHIPStream(c10::hip::getStreamFromExternal(static_cast<hipStream_t>(stream_), device_.index()));
+  }
+  ~OnStream() {
+    if (other_) c10::hip::setCurrentHIPStream(before_);
+  }
+  OnStream(const OnStream&) = delete;
+  OnStream& operator=(const OnStream&) = delete;
+  void* stream() const { return stream_; }
+  Tensor workspace(const Tensor* given, size_t need) const {
+    if (given != nullptr) {
+      if (!given->is_cuda() || given->device() != device_ || !given->is_contiguous() || given->scalar_type() != at::kByte)
+        raise(PyExc_ValueError, "workspace must be a contiguous uint8 tensor on the call's device");
+      return *given;
+    }
+    // (a graph's calls run whenever it is replayed: they share no scratch memory with calls outside it, or in another graph)
+    if (c10::hip::currentStreamCaptureStatusMayInitCtx() != c10::hip::CaptureStatus::None)
+      return at::empty({static_cast<int64_t>(std::max<size_t>(need, 256))}, at::TensorOptions().dtype(at::kByte).device(device_));
+    return shared_workspace(need, device_, stream_);
+  }
+
+ private:
+  c10::DeviceGuard guard_;
+  at::Device device_;
+  c10::hip::HIPStream before_;
+  void* stream_;
+  bool other_;
+};
+
+const Tensor& storage_type(const Tensor& t) {
+  if (t.scalar_type() != at::kFloat && t.scalar_type() != at::kBFloat16) raise(PyExc_TypeError, "unsupported tensor dtype: float32 or bfloat16 is expected");
+  return t;
+}
+// [rows, heads, dh] with rows that lie a stride of their own apart
+int64_t heads_stride(const Tensor& t, const Tensor& like, const char* what) {
+  want_dims(t, 3, what);
+  if (!t.is_cuda()) raise(PyExc_ValueError, "tensors must be CUDA tensors");
+  if (t.scalar_type() != like.scalar_type() || t.device() != like.device()) raise(PyExc_ValueError, "tensors must share dtype and device");
+  const int64_t heads = t.size(1), dh = t.size(2);
+  if (t.numel() == 0) return heads * dh;
+  if ((dh > 1 && t.stride(2) != 1) || (heads > 1 && t.stride(1) != dh)) raise(PyExc_ValueError, "the heads of a row must be contiguous");
+  return t.size(0) > 1 ? t.stride(0) : heads * dh;
+}
+void same_sizes(const Tensor& t, at::IntArrayRef sizes, const char* what) {
+  if (t.sizes() != sizes) raise(PyExc_ValueError, what);
+}
+// A contiguous tensor of the given sizes and type beside `like`, or a new one.
+Tensor plain(const Tensor* given, at::IntArrayRef sizes, const Tensor& like, at::ScalarType type, const char* what) {
+  if (given == nullptr) return at::empty(sizes, like.options().dtype(type));
+  if (given->sizes() != sizes || given->scalar_type() != type || given->device() != like.device() || !given->is_contiguous()) raise(PyExc_ValueError, what);
+  return *given;
+}
+const int32_t* index_tensor(const Tensor* t, int64_t entries, const Tensor& like, const char* what) {
+  if (t == nullptr) return nullptr;
+  if (t->scalar_type() != at::kInt || t->device() != like.device() || t->numel() != entries || !t->is_contiguous()) raise(PyExc_ValueError, what);
+  return ints(t);
+}
+// The new tensor for an output of [rows, heads, dh], or the given one with its stride.
+struct HeadsOut {
+  Tensor t;
+  int64_t stride;
+  HeadsOut(const Tensor* given, at::IntArrayRef sizes, const Tensor& like)
+      : t(given != nullptr ? *given : at::empty(sizes, like.options())), stride(heads_stride(t, like, "outputs must be [rows, heads, dh]")) {
+    same_sizes(t, sizes, "an output has other sizes than its tensor");
+  }
+};
+int32_t count32(int64_t n, const char* what) {
+  if (n > INT32_MAX) raise(PyExc_ValueError, what);
+  return static_cast<int32_t>(n);
+}
+PyObject* tuple_of(std::initializer_list<const Tensor*> tensors) {
+  PyObject* t = PyTuple_New(static_cast<Py_ssize_t>(tensors.size()));
+  if (t == nullptr) throw PyFailed{};
+  Py_ssize_t i = 0;
+  for (const Tensor* x : tensors) {
+    if (x == nullptr || !x->defined()) Py_INCREF(Py_None);
+    PyTuple_SET_ITEM(t, i++, x == nullptr || !x->defined() ? Py_None : wrap(*x));
+  }
+  return t;
+}
+
+// What both directions of the norms and rotation check.
+struct RotaryCall {
+  int32_t hq, hk, dh, code;
+  int64_t rows, q_stride, k_stride = 0;
+  const int32_t* positions;
+  RotaryCall(const Tensor& Q, const Tensor* K, const Tensor* gq, const Tensor* gk, const Tensor* pos) {
+    storage_type(Q);
+    q_stride = heads_stride(Q, Q, "Q must be [rows, hq, dh]");
+    rows = Q.size(0), hq = dim(Q, 1), dh = dim(Q, 2), hk = K != nullptr ? dim(*K, 1) : 0, code = dtype_code(Q);
+    if (K != nullptr) {
+      k_stride = heads_stride(*K, Q, "K must be [rows, hk, dh]");
+      if (K->size(0) != rows || K->size(2) != dh) raise(PyExc_ValueError, "Q and K must have the same rows and head width");
+    }
+    for (const Tensor* g : {gq, gk})
+      if (g != nullptr && (g->scalar_type() != Q.scalar_type() || g->device() != Q.device() || g->numel() != dh || !g->is_contiguous()))
+        raise(PyExc_ValueError, "gamma must be a contiguous [dh] tensor of the heads' dtype and device");
+    positions = index_tensor(pos, rows, Q, "positions must be a contiguous CUDA int32 tensor of an entry for each row");
+  }
+};
+
+// (Q, K, gamma_q, gamma_k, positions, base, eps, QO, KO, stream) -> (QO, KO or None)
+PyObject* norm_rotary(Args a) {
+  const Tensor *Q = a.tensor(), *K = a.tensor(false), *gq = a.tensor(false), *gk = a.tensor(false), *pos = a.tensor(false);
+  const float base = a.number(), eps = a.number();
+  const Tensor *QOin = a.tensor(false), *KOin = a.tensor(false);
+  const RotaryCall c(*Q, K, gq, gk, pos);
+  OnStream s(*Q, a.object());
+  const HeadsOut QO(QOin, Q->sizes(), *Q);
+  const HeadsOut KO(K != nullptr ? KOin : &QO.t, K != nullptr ? K->sizes() : Q->sizes(), *Q);
+  call(lime_norm_rotary, ptr(Q), c.q_stride, ptr(K), c.k_stride, ptr(gq), ptr(gk), c.positions, base, eps, ptr(&QO.t), QO.stride, ptr(&KO.t), KO.stride, c.rows,
+       c.hq, c.hk, c.dh, c.code, s.stream());
+  return tuple_of({&QO.t, K != nullptr ? &KO.t : nullptr});
+}
+
+// (dQO, dKO, Q, K, gamma_q, gamma_k, positions, base, eps, dQ, dK, workspace, stream) -> (dQ, dK, dgamma_q, dgamma_k)
+PyObject* norm_rotary_backward(Args a) {
+  const Tensor *dQO = a.tensor(), *dKO = a.tensor(false), *Q = a.tensor(), *K = a.tensor(false), *gq = a.tensor(false), *gk = a.tensor(false), *pos = a.tensor(false);
+  const float base = a.number(), eps = a.number();
+  const Tensor *dQin = a.tensor(false), *dKin = a.tensor(false), *workspace = a.tensor(false);
+  const RotaryCall c(*Q, K, gq, gk, pos);
+  if ((K == nullptr) != (dKO == nullptr)) raise(PyExc_ValueError, "K and dKO go together");
+  const int64_t dqo = heads_stride(*dQO, *Q, "dQO must be [rows, hq, dh]"), dko = K != nullptr ? heads_stride(*dKO, *Q, "dKO must be [rows, hk, dh]") : 0;
+  same_sizes(*dQO, Q->sizes(), "dQO must have Q's sizes");
+  if (K != nullptr) same_sizes(*dKO, K->sizes(), "dKO must have K's sizes");
+  OnStream s(*Q, a.object());
+  const HeadsOut dQ(dQin, Q->sizes(), *Q);
+  const HeadsOut dK(K != nullptr ? dKin : &dQ.t, K != nullptr ? K->sizes() : Q->sizes(), *Q);
+  Tensor dgq, dgk;
+  if (gq != nullptr) dgq = at::empty({c.dh}, Q->options());
+  if (gk != nullptr && K != nullptr) dgk = at::empty({c.dh}, Q->options());
+  const Tensor ws = s.workspace(workspace, lime_norm_rotary_backward_workspace_bytes(c.rows, c.dh));
+  call(lime_norm_rotary_backward, ptr(dQO), dqo, ptr(dKO), dko, ptr(Q), c.q_stride, ptr(K), c.k_stride, ptr(gq), ptr(gk), c.positions, base, eps, ptr(&dQ.t),
+       dQ.stride, ptr(&dK.t), dK.stride, dgq.defined() ? dgq.data_ptr() : nullptr, dgk.defined() ? dgk.data_ptr() : nullptr, c.rows, c.hq, c.hk, c.dh, c.code,
+       ws.data_ptr(), static_cast<size_t>(ws.numel()), s.stream());
+  return tuple_of({&dQ.t, K != nullptr ? &dK.t : nullptr, &dgq, &dgk});
+}
+
+// What both directions of the attention check.
+struct SequenceCall {
+  lime_sequences where{};
+  int32_t hq, hk, dh, code;
+  int64_t q_stride, k_stride, v_stride;
+  SequenceCall(const Tensor& Q, const Tensor& K, const Tensor& V, const Tensor& q_offsets, const Tensor& k_offsets, int32_t max_q, int32_t max_k,
+               const Tensor* q_lens, const Tensor* k_lens) {
+    storage_type(Q);
+    q_stride = heads_stride(Q, Q, "Q must be [q_rows, hq, dh]"), k_stride = heads_stride(K, Q, "K must be [k_rows, hk, dh]");
+    v_stride = heads_stride(V, Q, "V must be [k_rows, hk, dh]");
+    if (K.sizes() != V.sizes() || K.size(2) != Q.size(2)) raise(PyExc_ValueError, "K and V must have the same sizes, and Q's head width");
+    hq = dim(Q, 1), hk = dim(K, 1), dh = dim(Q, 2), code = dtype_code(Q);
+    if (q_offsets.numel() < 2) raise(PyExc_ValueError, "q_offsets must have an entry for each user and one more");
+    const int64_t B = q_offsets.numel() - 1;
+    where.q_offsets = index_tensor(&q_offsets, B + 1, Q, "q_offsets must be a contiguous CUDA int32 tensor");
+    where.k_offsets = index_tensor(&k_offsets, B + 1, Q, "k_offsets must be a contiguous CUDA int32 tensor of q_offsets' entries");
+    where.q_lens = index_tensor(q_lens, B, Q, "q_lens must be a contiguous CUDA int32 tensor of an entry for each user");
+    where.k_lens = index_tensor(k_lens, B, Q, "k_lens must be a contiguous CUDA int32 tensor of an entry for each user");
+    where.q_rows = Q.size(0), where.k_rows = K.size(0), where.B = count32(B, "too many users"), where.max_q = max_q, where.max_k = max_k;
+  }
+};
+
+// (Q, K, V, q_offsets, k_offsets, max_q, max_k, scale, q_lens, k_lens, causal, O, lse, workspace, stream) -> (O, lse)
+PyObject* sequence_attention(Args a) {
+  const Tensor *Q = a.tensor(), *K = a.tensor(), *V = a.tensor(), *qo = a.tensor(), *ko = a.tensor();
+  const int32_t max_q = a.integer(), max_k = a.integer();
+  const float scale = a.number();
+  const Tensor *ql = a.tensor(false), *kl = a.tensor(false);
+  const bool causal = a.truth();
+  const Tensor *Oin = a.tensor(false), *lsein = a.tensor(false), *workspace = a.tensor(false);
+  const SequenceCall c(*Q, *K, *V, *qo, *ko, max_q, max_k, ql, kl);
+  OnStream s(*Q, a.object());
+  const Tensor O = plain(Oin, Q->sizes(), *Q, Q->scalar_type(), "O must be a contiguous tensor of Q's sizes and dtype");
+  const Tensor lse = plain(lsein, {Q->size(0), Q->size(1)}, *Q, at::kFloat, "lse must be a contiguous fp32 tensor [q_rows, hq]");
+  const Tensor ws = s.workspace(workspace, lime_sequence_attention_workspace_bytes(&c.where, c.hq, c.hk, c.dh, c.code, 0));
+  call(lime_sequence_attention, &c.where, ptr(Q), c.q_stride, ptr(K), c.k_stride, ptr(V), c.v_stride, ptr(&O), static_cast<float*>(ptr(&lse)), c.hq, c.hk, c.dh,
+       scale, static_cast<int32_t>(causal), c.code, ws.data_ptr(), static_cast<size_t>(ws.numel()), s.stream());
+  return tuple_of({&O, &lse});
+}
+
+// (dO, Q, K, V, O, lse, q_offsets, k_offsets, max_q, max_k, scale, q_lens, k_lens, causal, dQ, dK, dV, workspace, stream) -> (dQ, dK, dV)
+PyObject* sequence_attention_backward(Args a) {
+  const Tensor *dO = a.tensor(), *Q = a.tensor(), *K = a.tensor(), *V = a.tensor(), *O = a.tensor(), *lse = a.tensor(), *qo = a.tensor(), *ko = a.tensor();
+  const int32_t max_q = a.integer(), max_k = a.integer();
+  const float scale = a.number();
+  const Tensor *ql = a.tensor(false), *kl = a.tensor(false);
+  const bool causal = a.truth();
+  const Tensor *dQin = a.tensor(false), *dKin = a.tensor(false), *dVin = a.tensor(false), *workspace = a.tensor(false);
+  const SequenceCall c(*Q, *K, *V, *qo, *ko, max_q, max_k, ql, kl);
+  plain(dO, Q->sizes(), *Q, Q->scalar_type(), "dO must be a contiguous tensor of Q's sizes and dtype");
+  plain(O, Q->sizes(), *Q, Q->scalar_type(), "O must be a contiguous tensor of Q's sizes and dtype");
+  plain(lse, {Q->size(0), Q->size(1)}, *Q, at::kFloat, "lse must be a contiguous fp32 tensor [q_rows, hq]");
+  OnStream s(*Q, a.object());
+  const HeadsOut dQ(dQin, Q->sizes(), *Q), dK(dKin, K->sizes(), *Q), dV(dVin, V->sizes(), *Q);
+  const Tensor ws = s.workspace(workspace, lime_sequence_attention_workspace_bytes(&c.where, c.hq, c.hk, c.dh, c.code, 1));
+  call(lime_sequence_attention_backward, &c.where, ptr(dO), ptr(Q), c.q_stride, ptr(K), c.k_stride, ptr(V), c.v_stride, ptr(O), static_cast<const float*>(ptr(lse)),
+       ptr(&dQ.t), dQ.stride, ptr(&dK.t), dK.stride, ptr(&dV.t), dV.stride, c.hq, c.hk, c.dh, scale, static_cast<int32_t>(causal), c.code, ws.data_ptr(),
+       static_cast<size_t>(ws.numel()), s.stream());
+  return tuple_of({&dQ.t, &dK.t, &dV.t});
+}
+
+// What both directions of the loss check.
+struct CatalogueCall {
+  int64_t rows;
+  int32_t items, d, code;
+  const int32_t* targets;
+  CatalogueCall(const Tensor& X, const Tensor& W, const Tensor& t) {
+    const Tensor& like = check({&X, &W});
+    want_dims(X, 2, "X must be [rows, d]"), want_dims(W, 2, "W must be [n_items, d]");
+    if (X.size(1) != W.size(1)) raise(PyExc_ValueError, "X and W must have the same width");
+    rows = X.size(0), items = count32(W.size(0), "too many items"), d = dim(X, 1), code = dtype_code(like);
+    targets = index_tensor(&t, rows, X, "targets must be a contiguous CUDA int32 tensor of an entry for each row");
+  }
+};
+
+// (X, W, targets, scale, loss, lse, workspace, stream) -> (loss, lse)
+PyObject* catalogue_loss(Args a) {
+  const Tensor *X = a.tensor(), *W = a.tensor(), *targets = a.tensor();
+  const float scale = a.number();
+  const Tensor *lossin = a.tensor(false), *lsein = a.tensor(false), *workspace = a.tensor(false);
+  const CatalogueCall c(*X, *W, *targets);
+  OnStream s(*X, a.object());
+  const Tensor loss = plain(lossin, {c.rows}, *X, at::kFloat, "loss must be a contiguous fp32 tensor [rows]");
+  const Tensor lse = plain(lsein, {c.rows}, *X, at::kFloat, "lse must be a contiguous fp32 tensor [rows]");
+  const Tensor ws = s.workspace(workspace, lime_catalogue_loss_workspace_bytes(c.rows, c.items, c.d, c.code, 0));
+  call(lime_catalogue_loss, ptr(X), ptr(W), c.targets, static_cast<float*>(ptr(&loss)), static_cast<float*>(ptr(&lse)), c.rows, c.items, c.d, scale, c.code,
+       ws.data_ptr(), static_cast<size_t>(ws.numel()), s.stream());
+  return tuple_of({&loss, &lse});
+}
+
+// (dloss, X, W, targets, lse, scale, dX, dW, workspace, stream) -> (dX, dW)
+PyObject* catalogue_loss_backward(Args a) {
+  const Tensor *dloss = a.tensor(), *X = a.tensor(), *W = a.tensor(), *targets = a.tensor(), *lse = a.tensor();
+  const float scale = a.number();
+  const Tensor *dXin = a.tensor(false), *dWin = a.tensor(false), *workspace = a.tensor(false);
+  const CatalogueCall c(*X, *W, *targets);
+  plain(dloss, {c.rows}, *X, at::kFloat, "dloss must be a contiguous fp32 tensor [rows]");
+  plain(lse, {c.rows}, *X, at::kFloat, "lse must be a contiguous fp32 tensor [rows]");
+  OnStream s(*X, a.object());
+  const Tensor dX = plain(dXin, X->sizes(), *X, X->scalar_type(), "dX must be a contiguous tensor of X's sizes and dtype");
+  const Tensor dW = plain(dWin, W->sizes(), *X, X->scalar_type(), "dW must be a contiguous tensor of W's sizes and dtype");
+  const Tensor ws = s.workspace(workspace, lime_catalogue_loss_workspace_bytes(c.rows, c.items, c.d, c.code, 1));
+  call(lime_catalogue_loss_backward, static_cast<const float*>(ptr(dloss)), ptr(X), ptr(W), c.targets, static_cast<const float*>(ptr(lse)), ptr(&dX), ptr(&dW), c.rows,
+       c.items, c.d, scale, c.code, ws.data_ptr(), static_cast<size_t>(ws.numel()), s.stream());
+  return tuple_of({&dX, &dW});
+}
+
 // (bytes, device index, stream or None) -> the shared workspace of that device and stream
 PyObject* workspace(Args a) {
   const size_t bytes = PyLong_AsSize_t(a.object());
@@ -493,6 +746,8 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 PyMethodDef g_methods[] = {LIME_ENTRY(history, 14), LIME_ENTRY(xor_layers, 13), LIME_ENTRY(score_candidates, 11), LIME_ENTRY(target_attention, 11),
                            LIME_ENTRY(score_cached, 7), LIME_ENTRY(history_prepared, 10), LIME_ENTRY(candidates_prepared, 9),
                            LIME_ENTRY(request, 20), LIME_ENTRY(request_prepared, 14), LIME_ENTRY(xor_backward, 13), LIME_ENTRY(scores, 8),
+                           LIME_ENTRY(norm_rotary, 10), LIME_ENTRY(norm_rotary_backward, 13), LIME_ENTRY(sequence_attention, 15),
+                           LIME_ENTRY(sequence_attention_backward, 19), LIME_ENTRY(catalogue_loss, 8), LIME_ENTRY(catalogue_loss_backward, 10),
                            LIME_ENTRY(workspace, 3), LIME_ENTRY(set_error_type, 1), {nullptr, nullptr, 0, nullptr}};
 #undef LIME_ENTRY
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_lime_torch", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};

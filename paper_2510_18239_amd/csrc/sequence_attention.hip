@@ -1,0 +1,267 @@
+// Softmax attention over packed sequences with grouped heads:
+//   O_i = sum_j p_ij V_j,   p_ij = exp(scale <Q_i, K_j> - lse_i),   lse_i = log sum_j exp(scale <Q_i, K_j>)   over the keys j that i sees.
+// One pass over the keys with a running maximum m and sum l (everything in base 2): S^T = K Q^T block by block, so that a lane
+// holds one query row and the softmax's statistics are the lane's own and its partner's; p = exp2(S c - m) rounded to the storage
+// type is, as it stands, the operand of O^T += V^T P^T.  The rows of a workgroup are pairs (query, head of the group) that share a
+// key head, in memory order: a tile of keys and values is read once for a whole group, in a prompt as for a single query.
+#include <algorithm>
+
+#include "sequences.hpp"
+
+namespace lime {
+namespace {
+
+struct Args {
+  const void *q, *k, *v;
+  int64_t q_stride, k_stride, v_stride;  // elements
+  const int32_t *q_offsets, *q_lens, *k_offsets, *k_lens;
+  void* o;
+  float* lse;
+  float *part_o, *part_ml;  // splits > 1: [splits][B][hk][max_q group][padded dh], [...][2]
+  int64_t q_rows, k_rows;
+  int B, max_q, max_k, hq, hk, group, dh, tiles, splits, chunk;
+  float c;                  // |scale| log2 e
+  bool negate, pieces, causal, quads;
+};
+
+// The running maximum is raised, and what has been summed scaled down, only where a row's logits have outgrown it by more than
+// this (a factor of 2^8 in p, which neither fp32 sums nor the rounding of p mind): rarely after a row's first tiles.
+constexpr float kHeadroom = 8.f;
+
+// WAVES waves of 32 rows each; KEYS keys a step, STAGES steps' tiles in LDS (one in use, the others on their way).
+template <typename T, int DH, int WAVES, int KEYS, int STAGES>
+__global__ __launch_bounds__(WAVES * 64) void sequence_attention_kernel(Args a) {
+  using Shape = Tile<T, DH, KEYS>;
+  using Loader = TileLoader<T, DH, KEYS, WAVES>;
+  constexpr int KB = KEYS / 32, OB = DH / 32, NK = DH / 16, ROWS = 32 * WAVES;
+  extern __shared__ __align__(1024) unsigned char smem[];  // [STAGES][keys, values]
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
+  // users and key heads fastest: the workgroups of one of them, which read the same keys, land on the same XCD where their number
+  // is a multiple of eight; last tiles of rows first, under a causal mask the longest
+  const int pairs = a.B * a.hk, pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
+  const int split = rest % a.splits, tile = a.tiles - 1 - rest / a.splits;
+  const int b = pair / a.hk, kv = pair % a.hk;
+  const Span qs = span_of(a.q_offsets, a.q_lens, b, a.q_rows, a.max_q), ks = span_of(a.k_offsets, a.k_lens, b, a.k_rows, a.max_k);
+  const int r0 = tile * ROWS, slot_rows = qs.slot * a.group, used_rows = qs.used * a.group;
+  if (r0 >= slot_rows) return;
+  // this lane's row
+  const int r = r0 + 32 * wave + n, query = r / a.group, head = kv * a.group + r % a.group;
+  const bool live = r < used_rows;
+  const int limit = live ? keys_seen(query, qs.used, ks.used, a.causal) : 0;
+  // the furthest any row of the wave, of the workgroup, sees, and the least that a live row of the wave does
+  auto last_limit = [&](int rows_end) { return rows_end > 0 ? keys_seen((rows_end - 1) / a.group, qs.used, ks.used, a.causal) : 0; };
+  const int w0 = r0 + 32 * wave, wave_most = w0 < used_rows ? last_limit(min(w0 + 32, used_rows)) : 0;
+  const int wave_least = w0 + 32 <= used_rows ? keys_seen(w0 / a.group, qs.used, ks.used, a.causal) : 0;
+  const int most = r0 < used_rows ? last_limit(min(r0 + ROWS, used_rows)) : 0;
+  const int k_begin = split * a.chunk, k_end = a.splits > 1 ? min(most, k_begin + a.chunk) : most;
+  const int steps = k_end > k_begin ? (k_end - k_begin + KEYS - 1) / KEYS : 0;
+
+  const T* kp = static_cast<const T*>(a.k) + (ks.start + k_begin) * a.k_stride + kv * a.dh;
+  const T* vp = static_cast<const T*>(a.v) + (ks.start + k_begin) * a.v_stride + kv * a.dh;
+  const unsigned width = a.dh * sizeof(T);
+  const Rows km{kp, static_cast<unsigned>(a.k_stride * sizeof(T)), width, a.pieces}, vm{vp, static_cast<unsigned>(a.v_stride * sizeof(T)), width, a.pieces};
+  Loader kl, vl;
+  kl.init(km, tid), vl.init(vm, tid);
+  auto stage = [&](int i) { return smem + (i % STAGES) * 2 * Shape::kBytes; };
+  auto ask = [&](int i) {
+    kl.issue(km, i * KEYS, k_end - k_begin, stage(i), tid);
+    vl.issue(vm, i * KEYS, k_end - k_begin, stage(i) + Shape::kBytes, tid);
+  };
+#pragma unroll
+  for (int i = 0; i < STAGES - 1; ++i)
+    if (i < steps) ask(i);
+
+  Fragment<T> q[NK];
+  const T* qp = static_cast<const T*>(a.q) + (qs.start + query) * a.q_stride + head * a.dh;
+  load_row<T, DH>(qp, width, a.pieces, live, g, q);
+  if (a.negate) {
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) q[kk] = -q[kk];
+  }
+  f32x16 o[OB];
+#pragma unroll
+  for (int ob = 0; ob < OB; ++ob) o[ob] = zero_block();
+  float m = -INFINITY, l = 0.f;  // of this lane's row; l of the lane half's keys
+
+  for (int i = 0; i < steps; ++i) {
+    if (STAGES > 2 && i + STAGES - 1 <= steps) wait_lds_loads<(STAGES - 2) * 2 * Loader::kLoads>();
+    else wait_lds_loads<0>();
+    lds_barrier();  // everyone's part of this step's tiles is there, and everyone is done with the last step's
+    if (i + STAGES - 1 < steps) ask(i + STAGES - 1);
+    const int key0 = k_begin + i * KEYS;
+    if (key0 >= wave_most) continue;
+    const unsigned char *kt = stage(i), *vt = kt + Shape::kBytes;
+    f32x16 s[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      s[kb] = zero_block();
+#pragma unroll
+      for (int kk = 0; kk < NK; ++kk) s[kb] = mma16(Shape::row_fragment(kt, 32 * kb, kk, lane), q[kk], s[kb]);
+    }
+    if (key0 + KEYS > wave_least) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int x = 0; x < 16; ++x)
+          if (key0 + 32 * kb + block_row(x, g) >= limit) s[kb][x] = -INFINITY;
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) top = fmaxf(top, s[kb][x]);
+    top = pair_max(top) * a.c;
+    if (__any(top > m + kHeadroom)) {
+      const float to = fmaxf(m, top), f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
+      m = to, l *= f;
+#pragma unroll
+      for (int ob = 0; ob < OB; ++ob)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) o[ob][x] *= f;
+    }
+    const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        s[kb][x] = __builtin_amdgcn_exp2f(fmaf(s[kb][x], a.c, -base));
+        l += s[kb][x];
+      }
+#pragma unroll
+      for (int f = 0; f < 2; ++f) {
+        const Fragment<T> p = half_fragment<T>(s[kb], f);
+#pragma unroll
+        for (int ob = 0; ob < OB; ++ob) o[ob] = mma16(Shape::column_fragment(vt, 32 * kb + 16 * f, 32 * ob, lane), p, o[ob]);
+      }
+    }
+  }
+  l = pair_sum(l);
+  if (r >= slot_rows) return;
+  if (a.splits > 1) {
+    const int64_t at = (static_cast<int64_t>(split) * pairs + pair) * (static_cast<int64_t>(a.max_q) * a.group) + r;
+#pragma unroll
+    for (int ob = 0; ob < OB; ++ob) store_block(a.part_o + at * DH, o[ob], 1.f, 32 * ob, DH, true, g);
+    if (g == 0) a.part_ml[at * 2] = m, a.part_ml[at * 2 + 1] = l;
+    return;
+  }
+  const float inverse = l == 0.f ? 0.f : 1.f / l;
+  const int64_t row = (qs.start + query) * a.hq + head;
+  T* op = static_cast<T*>(a.o) + row * a.dh;
+#pragma unroll
+  for (int ob = 0; ob < OB; ++ob) store_block(op, o[ob], inverse, 32 * ob, a.dh, a.quads, g);
+  if (a.lse != nullptr && g == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// The chunks' states of a row folded in ascending order; DH / 4 lanes a row.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void sequence_attention_merge_kernel(Args a) {
+  constexpr int LANES = DH / 4, PER = 256 / LANES;
+  const int tid = threadIdx.x, t = tid % LANES, pairs = a.B * a.hk;
+  const int pair = blockIdx.x % pairs, b = pair / a.hk, kv = pair % a.hk;
+  const int r = blockIdx.x / pairs * PER + tid / LANES;
+  const Span qs = span_of(a.q_offsets, a.q_lens, b, a.q_rows, a.max_q);
+  if (r >= qs.slot * a.group) return;
+  const int64_t each = static_cast<int64_t>(a.max_q) * a.group, step = pairs * each, at = pair * each + r;
+  float m = -INFINITY;
+  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_ml[(at + s * step) * 2]);
+  const float base = m == -INFINITY ? 0.f : m;
+  float l = 0.f;
+  f32x4 o = {0, 0, 0, 0};
+  for (int s = 0; s < a.splits; ++s) {
+    const float f = __builtin_amdgcn_exp2f(a.part_ml[(at + s * step) * 2] - base);
+    l = fmaf(f, a.part_ml[(at + s * step) * 2 + 1], l);
+    const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_o + (at + s * step) * DH + 4 * t);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] = fmaf(f, x[j], o[j]);
+  }
+  const float inverse = l == 0.f ? 0.f : 1.f / l;
+  const int64_t row = (qs.start + r / a.group) * a.hq + kv * a.group + r % a.group;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (4 * t + j < a.dh) store_as(static_cast<T*>(a.o) + row * a.dh + 4 * t + j, o[j] * inverse);
+  if (a.lse != nullptr && t == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+struct Plan {
+  int waves, keys, tiles, splits, chunk, dh;  // dh: padded
+  size_t o_bytes, bytes;
+};
+
+// Rows that one wave holds take a workgroup of one wave.  Where the tiles of rows are too few to fill the chip, the keys are cut
+// into chunks as well, none shorter than 256 keys.
+Plan plan_of(const SequenceAttention& a) {
+  const int64_t B = a.B, hk = a.hk, max_k = std::max(a.max_k, 1), rows = std::max<int64_t>(a.max_q, 1) * (a.hq / a.hk);
+  const int dh = a.dh, dtype = a.dtype;
+  Plan p{};
+  p.dh = dh <= 32 ? 32 : dh <= 64 ? 64 : 128;
+  p.waves = rows <= 32 ? 1 : 4;
+  p.keys = dtype == 1 ? 64 : 32;
+  p.tiles = static_cast<int>((rows + 32 * p.waves - 1) / (32 * p.waves));
+  const int64_t groups = B * hk * p.tiles;
+  const int64_t want = (p.waves == 1 ? 8 : 2) * static_cast<int64_t>(compute_units());
+  int64_t splits = groups >= want ? 1 : std::min((want + groups - 1) / groups, (max_k + 255) / 256);
+  int64_t chunk = (max_k + splits - 1) / splits;
+  chunk = (chunk + p.keys - 1) / p.keys * p.keys;
+  splits = (max_k + chunk - 1) / chunk;
+  p.chunk = static_cast<int>(std::min<int64_t>(chunk, (int64_t{1} << 31) - 1)), p.splits = static_cast<int>(splits);
+  if (p.splits > 1) {
+    const size_t states = static_cast<size_t>(p.splits) * B * hk * rows;
+    p.o_bytes = align_up(states * p.dh * sizeof(float));
+    p.bytes = p.o_bytes + align_up(states * 2 * sizeof(float));
+  }
+  return p;
+}
+
+template <typename T, int DH, int WAVES, int KEYS, int STAGES>
+hipError_t launch(const Args& a, int64_t blocks, hipStream_t s) {
+  constexpr int lds = STAGES * 2 * Tile<T, DH, KEYS>::kBytes;
+  static PerDevice granted;
+  const auto kernel = sequence_attention_kernel<T, DH, WAVES, KEYS, STAGES>;
+  if (hipError_t e = allow_lds(granted, reinterpret_cast<const void*>(kernel), lds); e != hipSuccess) return e;
+  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks)), dim3(WAVES * 64), lds, s, a);
+  return hipGetLastError();
+}
+
+template <typename T, int DH>
+hipError_t run(const Args& a, const Plan& p, hipStream_t s) {
+  constexpr int KEYS = sizeof(T) == 2 ? 64 : 32;
+  const int64_t pairs = static_cast<int64_t>(a.B) * a.hk, blocks = pairs * a.tiles * a.splits;
+  hipError_t e = p.waves == 1 ? launch<T, DH, 1, KEYS, 2>(a, blocks, s) : launch<T, DH, 4, KEYS, 2>(a, blocks, s);
+  if (e != hipSuccess || a.splits == 1) return e;
+  const int64_t rows = static_cast<int64_t>(a.max_q) * a.group, per = 256 / (DH / 4);
+  hipLaunchKernelGGL((sequence_attention_merge_kernel<T, DH>), dim3(static_cast<unsigned>(pairs * ((rows + per - 1) / per))), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+bool multiple(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+}  // namespace
+
+bool sequence_attention_fits(const SequenceAttention& a) {  // 2^32 work items a launch
+  const int64_t rows = static_cast<int64_t>(a.max_q) * (a.hq / a.hk), pairs = static_cast<int64_t>(a.B) * a.hk;
+  if (rows >= (int64_t{1} << 31) - 128 || pairs >= (int64_t{1} << 24)) return false;
+  const Plan p = plan_of(a);
+  return pairs * p.tiles * p.splits < (int64_t{1} << 26) / p.waves && (p.splits == 1 || pairs * ((rows + 7) / 8) < (int64_t{1} << 24));
+}
+
+size_t sequence_attention_workspace(const SequenceAttention& a) { return std::max<size_t>(plan_of(a).bytes, 256); }
+
+hipError_t sequence_attention(const SequenceAttention& x, void* workspace, hipStream_t s) {
+  const Plan p = plan_of(x);
+  const size_t e = x.dtype == 1 ? 2 : 4;
+  Args a{};
+  a.q = x.Q, a.k = x.K, a.v = x.V, a.q_stride = x.q_stride, a.k_stride = x.k_stride, a.v_stride = x.v_stride;
+  a.q_offsets = x.q_offsets, a.q_lens = x.q_lens, a.k_offsets = x.k_offsets, a.k_lens = x.k_lens;
+  a.o = x.O, a.lse = x.lse, a.q_rows = x.q_rows, a.k_rows = x.k_rows;
+  a.part_o = static_cast<float*>(workspace), a.part_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.o_bytes);
+  a.B = x.B, a.max_q = x.max_q, a.max_k = x.max_k, a.hq = x.hq, a.hk = x.hk, a.group = x.hq / x.hk, a.dh = x.dh;
+  a.tiles = p.tiles, a.splits = p.splits, a.chunk = p.chunk;
+  a.c = std::max(fabsf(x.scale) * kLog2e, 1e-37f), a.negate = x.scale < 0.f, a.causal = x.causal != 0;
+  a.pieces = multiple(x.Q, 16) && multiple(x.K, 16) && multiple(x.V, 16) && x.dh * e % 16 == 0 && x.q_stride * e % 16 == 0 &&
+             x.k_stride * e % 16 == 0 && x.v_stride * e % 16 == 0;
+  a.quads = x.dh % 4 == 0 && multiple(x.O, 4 * e);
+  if (x.dtype == 1) return p.dh == 32 ? run<bf16_t, 32>(a, p, s) : p.dh == 64 ? run<bf16_t, 64>(a, p, s) : run<bf16_t, 128>(a, p, s);
+  return p.dh == 32 ? run<float, 32>(a, p, s) : p.dh == 64 ? run<float, 64>(a, p, s) : run<float, 128>(a, p, s);
+}
+
+}  // namespace lime

@@ -1,0 +1,306 @@
+// Gradients of the attention over packed sequences, with the attention matrix recomputed from the forward pass's lse: for G = dL/dO,
+//   p_ij = exp(scale <Q_i, K_j> - lse_i),  D_i = <G_i, O_i>,  e_ij = p_ij (<G_i, V_j> - D_i):
+//   dQ_i = scale sum_j e_ij K_j,   dK_j = scale sum_i e_ij Q_i,   dV_j = sum_i p_ij G_i   (i over all heads that share the key head).
+// Two kernels, each with one side's rows and sums in registers while the other side's tiles stream past, so that every sum has one
+// owner and one order (no atomics): the first holds queries (rows as in the forward pass) and also leaves D and lse, by head, for
+// the second, which holds keys.  Seven products of the tiles where a kernel that kept both sides' sums would do five: the sums of
+// the other side would have to meet in memory.  p and e are rounded to the storage type, as operands of the last products.
+#include <algorithm>
+
+#include "sequences.hpp"
+
+namespace lime {
+namespace {
+
+struct Args {
+  const void *q, *k, *v, *o, *go;
+  int64_t q_stride, k_stride, v_stride, dq_stride, dk_stride, dv_stride;  // elements
+  const int32_t *q_offsets, *q_lens, *k_offsets, *k_lens;
+  const float* lse;
+  float *lse2, *delta;  // [hq][q_rows]: lse log2 e, D
+  void *dq, *dk, *dv;
+  int64_t q_rows, k_rows;
+  int B, max_q, max_k, hq, hk, group, dh, tiles;
+  float scale;
+  bool pieces, causal, quads;
+};
+
+template <typename T, int DH, int WAVES, int KEYS>
+__global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args a) {
+  using Shape = Tile<T, DH, KEYS>;
+  using Loader = TileLoader<T, DH, KEYS, WAVES>;
+  constexpr int KB = KEYS / 32, OB = DH / 32, NK = DH / 16, ROWS = 32 * WAVES;
+  extern __shared__ __align__(1024) unsigned char smem[];  // [2][keys, values]
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
+  const int pairs = a.B * a.hk, pair = blockIdx.x % pairs, tile = a.tiles - 1 - static_cast<int>(blockIdx.x) / pairs;
+  const int b = pair / a.hk, kv = pair % a.hk;
+  const Span qs = span_of(a.q_offsets, a.q_lens, b, a.q_rows, a.max_q), ks = span_of(a.k_offsets, a.k_lens, b, a.k_rows, a.max_k);
+  const int r0 = tile * ROWS, slot_rows = qs.slot * a.group, used_rows = qs.used * a.group;
+  if (r0 >= slot_rows) return;
+  const int r = r0 + 32 * wave + n, query = r / a.group, head = kv * a.group + r % a.group;
+  const bool live = r < used_rows;
+  const int limit = live ? keys_seen(query, qs.used, ks.used, a.causal) : 0;
+  auto last_limit = [&](int rows_end) { return rows_end > 0 ? keys_seen((rows_end - 1) / a.group, qs.used, ks.used, a.causal) : 0; };
+  const int w0 = r0 + 32 * wave, wave_most = w0 < used_rows ? last_limit(min(w0 + 32, used_rows)) : 0;
+  const int wave_least = w0 + 32 <= used_rows ? keys_seen(w0 / a.group, qs.used, ks.used, a.causal) : 0;
+  const int most = r0 < used_rows ? last_limit(min(r0 + ROWS, used_rows)) : 0, steps = (most + KEYS - 1) / KEYS;
+
+  const unsigned width = a.dh * sizeof(T);
+  const Rows km{static_cast<const T*>(a.k) + ks.start * a.k_stride + kv * a.dh, static_cast<unsigned>(a.k_stride * sizeof(T)), width, a.pieces};
+  const Rows vm{static_cast<const T*>(a.v) + ks.start * a.v_stride + kv * a.dh, static_cast<unsigned>(a.v_stride * sizeof(T)), width, a.pieces};
+  Loader kl, vl;
+  kl.init(km, tid), vl.init(vm, tid);
+  auto ask = [&](int i) {
+    unsigned char* at = smem + i % 2 * 2 * Shape::kBytes;
+    kl.issue(km, i * KEYS, most, at, tid);
+    vl.issue(vm, i * KEYS, most, at + Shape::kBytes, tid);
+  };
+  // Few keys: all their tiles fit, and D comes from its other form, sum_j p_ij <G_i, V_j>.  <G_i, O_i> carries the rounding of O to
+  // the storage type, which is as large as the difference e_ij where a row sees two keys and fades with the square root of their
+  // number (two keys, bf16: gradients 5e-3 off from the rounded O, 2.6e-3 this way; past 128 keys the two are alike).
+  const bool resident = sizeof(T) == 2 && steps <= 2;
+  if (steps > 0) ask(0);
+  if (resident && steps > 1) ask(1);
+
+  const int64_t row = (qs.start + query) * a.hq + head;
+  Fragment<T> q[NK], go[NK];
+  load_row<T, DH>(static_cast<const T*>(a.q) + (qs.start + query) * a.q_stride + head * a.dh, width, a.pieces, live, g, q);
+  load_row<T, DH>(static_cast<const T*>(a.go) + row * a.dh, width, a.pieces, live, g, go);
+  const float c = a.scale * kLog2e, lse2 = live ? a.lse[row] * kLog2e : 0.f;
+  float delta = 0.f;
+  if (resident) {
+    wait_lds_loads<0>();
+    lds_barrier();
+    for (int kb = 0; kb < KB * steps; ++kb) {
+      const unsigned char *kt = smem + kb / KB * 2 * Shape::kBytes, *vt = kt + Shape::kBytes;
+      f32x16 s = zero_block(), e = zero_block();
+#pragma unroll
+      for (int kk = 0; kk < NK; ++kk) {
+        s = mma16(Shape::row_fragment(kt, kb % KB * 32, kk, lane), q[kk], s);
+        e = mma16(Shape::row_fragment(vt, kb % KB * 32, kk, lane), go[kk], e);
+      }
+#pragma unroll
+      for (int x = 0; x < 16; ++x)
+        if (32 * kb + block_row(x, g) < limit) delta = fmaf(__builtin_amdgcn_exp2f(fmaf(s[x], c, -lse2)), e[x], delta);
+    }
+    delta = pair_sum(delta);
+  } else {
+    Fragment<T> o[NK];
+    load_row<T, DH>(static_cast<const T*>(a.o) + row * a.dh, width, a.pieces, live, g, o);
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk)
+#pragma unroll
+      for (int t = 0; t < 8; ++t) delta = fmaf(static_cast<float>(go[kk][t]), static_cast<float>(o[kk][t]), delta);
+    delta = pair_sum(delta);
+  }
+  if (live && g == 0) {
+    const int64_t at = head * a.q_rows + qs.start + query;
+    a.lse2[at] = lse2, a.delta[at] = delta;
+  }
+  f32x16 dq[OB];
+#pragma unroll
+  for (int ob = 0; ob < OB; ++ob) dq[ob] = zero_block();
+
+  for (int i = 0; i < steps; ++i) {
+    wait_lds_loads<0>();
+    lds_barrier();
+    if (i + 1 < steps && !resident) ask(i + 1);
+    const int key0 = i * KEYS;
+    if (key0 >= wave_most) continue;
+    const unsigned char *kt = smem + i % 2 * 2 * Shape::kBytes, *vt = kt + Shape::kBytes;
+    const bool partial = key0 + KEYS > wave_least;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      f32x16 s = zero_block(), e = zero_block();
+#pragma unroll
+      for (int kk = 0; kk < NK; ++kk) {
+        s = mma16(Shape::row_fragment(kt, 32 * kb, kk, lane), q[kk], s);
+        e = mma16(Shape::row_fragment(vt, 32 * kb, kk, lane), go[kk], e);
+      }
+#pragma unroll
+      for (int x = 0; x < 16; ++x) e[x] = __builtin_amdgcn_exp2f(fmaf(s[x], c, -lse2)) * (e[x] - delta);
+      if (partial) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x)
+          if (key0 + 32 * kb + block_row(x, g) >= limit) e[x] = 0.f;
+      }
+#pragma unroll
+      for (int f = 0; f < 2; ++f) {
+        const Fragment<T> ef = half_fragment<T>(e, f);
+#pragma unroll
+        for (int ob = 0; ob < OB; ++ob) dq[ob] = mma16(Shape::column_fragment(kt, 32 * kb + 16 * f, 32 * ob, lane), ef, dq[ob]);
+      }
+    }
+  }
+  if (r >= slot_rows) return;
+  T* out = static_cast<T*>(a.dq) + (qs.start + query) * a.dq_stride + head * a.dh;
+#pragma unroll
+  for (int ob = 0; ob < OB; ++ob) store_block(out, dq[ob], a.scale, 32 * ob, a.dh, a.quads, g);
+}
+
+template <typename T, int DH, int STEP>
+__global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
+  using Shape = Tile<T, DH, STEP>;
+  using Loader = TileLoader<T, DH, STEP, 4>;
+  constexpr int QB = STEP / 32, OB = DH / 32, NK = DH / 16, KEYS = 128;
+  constexpr int kStage = 2 * Shape::kBytes + 512;          // queries, output gradients, lse2 [64], delta [64]
+  extern __shared__ __align__(1024) unsigned char smem[];  // [2] stages
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
+  // first keys first: under a causal mask most queries see them
+  const int pairs = a.B * a.hk, pair = blockIdx.x % pairs, tile = blockIdx.x / pairs;
+  const int b = pair / a.hk, kv = pair % a.hk;
+  const Span qs = span_of(a.q_offsets, a.q_lens, b, a.q_rows, a.max_q), ks = span_of(a.k_offsets, a.k_lens, b, a.k_rows, a.max_k);
+  const int j0 = tile * KEYS;
+  if (j0 >= ks.slot) return;
+  const int key = j0 + 32 * wave + n, shift = ks.used - qs.used;
+  const bool live = key < ks.used;
+  // the first query that sees this lane's key; that sees any of the wave's; that sees all of them
+  const int first = live ? (a.causal ? max(0, key - shift) : 0) : qs.used;
+  const int w0 = j0 + 32 * wave, wave_first = w0 < ks.used ? (a.causal ? max(0, w0 - shift) : 0) : qs.used;
+  const int wave_all = w0 + 32 <= ks.used ? (a.causal ? max(0, w0 + 31 - shift) : 0) : qs.used;
+  const int begin = (a.causal ? max(0, j0 - shift) : 0) / STEP * STEP;
+  const int each = j0 < ks.used && begin < qs.used ? (qs.used - begin + STEP - 1) / STEP : 0, steps = each * a.group;
+
+  const unsigned width = a.dh * sizeof(T);
+  Rows qm{static_cast<const T*>(a.q) + (qs.start + begin) * a.q_stride + kv * a.group * a.dh, static_cast<unsigned>(a.q_stride * sizeof(T)), width, a.pieces};
+  Rows gm{static_cast<const T*>(a.go) + ((qs.start + begin) * a.hq + kv * a.group) * a.dh, static_cast<unsigned>(a.hq * a.dh * sizeof(T)), width, a.pieces};
+  Loader ql, gl;
+  ql.init(qm, tid), gl.init(gm, tid);
+  // steps are asked for one head after the other
+  int ask_head = 0, ask_at = 0;
+  auto ask = [&](int i) {
+    unsigned char* at = smem + i % 2 * kStage;
+    const int count = qs.used - begin - ask_at;
+    ql.issue(qm, ask_at, qs.used - begin, at, tid);
+    gl.issue(gm, ask_at, qs.used - begin, at + Shape::kBytes, tid);
+    if (wave < 2) {
+      const float* from = (wave == 0 ? a.lse2 : a.delta) + (kv * a.group + ask_head) * a.q_rows + qs.start + begin + ask_at;
+      words_to_lds(from, min(count, STEP), reinterpret_cast<float*>(at + 2 * Shape::kBytes) + 64 * wave, lane);
+    }
+    ask_at += STEP;
+    if (ask_at >= each * STEP) {
+      ask_at = 0, ++ask_head;
+      qm.base = static_cast<const char*>(qm.base) + width, gm.base = static_cast<const char*>(gm.base) + width;
+    }
+  };
+  if (steps > 0) ask(0);
+
+  Fragment<T> k[NK], v[NK];
+  load_row<T, DH>(static_cast<const T*>(a.k) + (ks.start + key) * a.k_stride + kv * a.dh, width, a.pieces, live, g, k);
+  load_row<T, DH>(static_cast<const T*>(a.v) + (ks.start + key) * a.v_stride + kv * a.dh, width, a.pieces, live, g, v);
+  const float c = a.scale * kLog2e;
+  f32x16 dk[OB], dv[OB];
+#pragma unroll
+  for (int ob = 0; ob < OB; ++ob) dk[ob] = dv[ob] = zero_block();
+
+  int at = 0;  // this step's first query, from `begin`
+  for (int i = 0; i < steps; ++i) {
+    wait_lds_loads<0>();
+    lds_barrier();
+    if (i + 1 < steps) ask(i + 1);
+    const int q0 = begin + at;
+    at = at + STEP < each * STEP ? at + STEP : 0;
+    if (q0 + STEP <= wave_first) continue;
+    const unsigned char *qt = smem + i % 2 * kStage, *gt = qt + Shape::kBytes;
+    const float *lse2 = reinterpret_cast<const float*>(gt + Shape::kBytes), *delta = lse2 + 64;
+    const bool partial = q0 < wave_all || q0 + STEP > qs.used;
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      f32x16 p = zero_block(), e = zero_block();
+#pragma unroll
+      for (int kk = 0; kk < NK; ++kk) {
+        p = mma16(Shape::row_fragment(qt, 32 * qb, kk, lane), k[kk], p);
+        e = mma16(Shape::row_fragment(gt, 32 * qb, kk, lane), v[kk], e);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f32x4 l4 = *reinterpret_cast<const f32x4*>(lse2 + 32 * qb + 8 * j + 4 * g), d4 = *reinterpret_cast<const f32x4*>(delta + 32 * qb + 8 * j + 4 * g);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          p[4 * j + x] = __builtin_amdgcn_exp2f(fmaf(p[4 * j + x], c, -l4[x]));
+          e[4 * j + x] = p[4 * j + x] * (e[4 * j + x] - d4[x]);
+        }
+      }
+      if (partial) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+          const int query = q0 + 32 * qb + block_row(x, g);
+          if (query < first || query >= qs.used) p[x] = 0.f, e[x] = 0.f;
+        }
+      }
+#pragma unroll
+      for (int f = 0; f < 2; ++f) {
+        const Fragment<T> pf = half_fragment<T>(p, f), ef = half_fragment<T>(e, f);
+#pragma unroll
+        for (int ob = 0; ob < OB; ++ob) {
+          dv[ob] = mma16(Shape::column_fragment(gt, 32 * qb + 16 * f, 32 * ob, lane), pf, dv[ob]);
+          dk[ob] = mma16(Shape::column_fragment(qt, 32 * qb + 16 * f, 32 * ob, lane), ef, dk[ob]);
+        }
+      }
+    }
+  }
+  if (key >= ks.slot) return;
+  T* dk_row = static_cast<T*>(a.dk) + (ks.start + key) * a.dk_stride + kv * a.dh;
+  T* dv_row = static_cast<T*>(a.dv) + (ks.start + key) * a.dv_stride + kv * a.dh;
+#pragma unroll
+  for (int ob = 0; ob < OB; ++ob) {
+    store_block(dk_row, dk[ob], a.scale, 32 * ob, a.dh, a.quads, g);
+    store_block(dv_row, dv[ob], 1.f, 32 * ob, a.dh, a.quads, g);
+  }
+}
+
+template <typename T, int DH>
+hipError_t run(Args a, hipStream_t s) {
+  constexpr int STEP = sizeof(T) == 2 ? 64 : 32;
+  const int64_t pairs = static_cast<int64_t>(a.B) * a.hk;
+  if (a.max_q > 0) {
+    constexpr int lds = 4 * Tile<T, DH, STEP>::kBytes;
+    static PerDevice granted;
+    const auto kernel = sequence_attention_dq_kernel<T, DH, 4, STEP>;
+    if (hipError_t e = allow_lds(granted, reinterpret_cast<const void*>(kernel), lds); e != hipSuccess) return e;
+    a.tiles = static_cast<int>((static_cast<int64_t>(a.max_q) * a.group + 127) / 128);
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(pairs * a.tiles)), dim3(256), lds, s, a);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  if (a.max_k == 0) return hipSuccess;
+  constexpr int lds = 2 * (2 * Tile<T, DH, STEP>::kBytes + 512);
+  static PerDevice granted;
+  const auto kernel = sequence_attention_dkv_kernel<T, DH, STEP>;
+  if (hipError_t e = allow_lds(granted, reinterpret_cast<const void*>(kernel), lds); e != hipSuccess) return e;
+  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(pairs * ((a.max_k + 127) / 128))), dim3(256), lds, s, a);
+  return hipGetLastError();
+}
+
+bool multiple(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+}  // namespace
+
+bool sequence_attention_backward_fits(const SequenceAttention& a) {  // 2^32 work items a launch
+  const int64_t rows = static_cast<int64_t>(a.max_q) * (a.hq / a.hk), pairs = static_cast<int64_t>(a.B) * a.hk;
+  return rows < (int64_t{1} << 31) - 128 && pairs < (int64_t{1} << 24) && pairs * ((rows + 127) / 128) < (int64_t{1} << 24) &&
+         pairs * ((a.max_k + 127) / 128) < (int64_t{1} << 24);
+}
+
+size_t sequence_attention_backward_workspace(const SequenceAttention& a) { return std::max<size_t>(256, 2 * align_up(static_cast<size_t>(a.q_rows) * a.hq * sizeof(float))); }
+
+hipError_t sequence_attention_backward(const SequenceAttention& x, void* workspace, hipStream_t s) {
+  const size_t e = x.dtype == 1 ? 2 : 4;
+  Args a{};
+  a.q = x.Q, a.k = x.K, a.v = x.V, a.o = x.O, a.go = x.dO, a.dq = x.dQ, a.dk = x.dK, a.dv = x.dV, a.lse = x.lse;
+  a.q_stride = x.q_stride, a.k_stride = x.k_stride, a.v_stride = x.v_stride;
+  a.dq_stride = x.dq_stride, a.dk_stride = x.dk_stride, a.dv_stride = x.dv_stride;
+  a.q_offsets = x.q_offsets, a.q_lens = x.q_lens, a.k_offsets = x.k_offsets, a.k_lens = x.k_lens;
+  a.lse2 = static_cast<float*>(workspace);
+  a.delta = reinterpret_cast<float*>(static_cast<char*>(workspace) + align_up(static_cast<size_t>(x.q_rows) * x.hq * sizeof(float)));
+  a.q_rows = x.q_rows, a.k_rows = x.k_rows, a.B = x.B, a.max_q = x.max_q, a.max_k = x.max_k, a.hq = x.hq, a.hk = x.hk, a.group = x.hq / x.hk, a.dh = x.dh;
+  a.scale = x.scale, a.causal = x.causal != 0;
+  a.pieces = multiple(x.Q, 16) && multiple(x.K, 16) && multiple(x.V, 16) && multiple(x.O, 16) && multiple(x.dO, 16) && x.dh * e % 16 == 0 &&
+             x.q_stride * e % 16 == 0 && x.k_stride * e % 16 == 0 && x.v_stride * e % 16 == 0;
+  a.quads = x.dh % 4 == 0 && x.dq_stride % 4 == 0 && x.dk_stride % 4 == 0 && x.dv_stride % 4 == 0 && multiple(x.dQ, 4 * e) && multiple(x.dK, 4 * e) &&
+            multiple(x.dV, 4 * e);
+  const int dh = x.dh <= 32 ? 32 : x.dh <= 64 ? 64 : 128;
+  if (x.dtype == 1) return dh == 32 ? run<bf16_t, 32>(a, s) : dh == 64 ? run<bf16_t, 64>(a, s) : run<bf16_t, 128>(a, s);
+  return dh == 32 ? run<float, 32>(a, s) : dh == 64 ? run<float, 64>(a, s) : run<float, 128>(a, s);
+}
+
+}  // namespace lime

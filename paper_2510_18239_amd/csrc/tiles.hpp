@@ -1,0 +1,221 @@
+// Tiles of row-major matrices in LDS, streamed in straight from memory and read as matrix-instruction operands, for both
+// storage types: what the history encoder's attention and the catalogue loss are built from.
+//
+// A tile is ROWS rows of DH columns (the operand's own width rounded up; columns past it are zero).  Its 16-byte pieces are
+// permuted within a row by the row's number (swizzle), so that neither of the two ways it is read meets its own lanes in a bank:
+//   row_fragment     lane (n, g), slot t = tile[r0 + n][16 kk + 8g + t]            (the columns are summed)
+//   column_fragment  lane (n, g), slot t = tile[r0 + chain_k(g, t)][c0 + n]        (the rows are summed, in chained order)
+// A product's 32 x 32 accumulator, rounded to the storage type half by half (half_fragment), is the other operand of the
+// second: the two products of an attention step chain in registers.
+// fp32 tiles go through v_mfma_f32_32x32x2_f32, eight of which take the same 16-deep fragments one slot at a time.
+#pragma once
+
+#include <type_traits>
+
+#include "mfma.hpp"
+
+namespace lime {
+
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+template <typename T>
+using Fragment = std::conditional_t<std::is_same_v<T, float>, f32x8, bf16x8>;
+
+__device__ __forceinline__ f32x16 mma16(bf16x8 a, bf16x8 b, f32x16 c) { return mfma32(a, b, c); }
+__device__ __forceinline__ f32x16 mma16(f32x8 a, f32x8 b, f32x16 c) {
+#pragma unroll
+  for (int t = 0; t < 8; ++t) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[t], b[t], c, 0, 0, 0);
+  return c;
+}
+__device__ __forceinline__ f32x16 zero_block() {
+  f32x16 z;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) z[i] = 0.f;
+  return z;
+}
+// Registers 8f .. 8f + 7 of an accumulator as a fragment of the storage type (bf16: round to nearest even).
+template <typename T>
+__device__ __forceinline__ Fragment<T> half_fragment(const f32x16& d, int f) {
+  Fragment<T> r;
+#pragma unroll
+  for (int t = 0; t < 8; ++t) r[t] = static_cast<std::conditional_t<std::is_same_v<T, float>, float, __bf16>>(d[8 * f + t]);
+  return r;
+}
+// Row of a 32 x 32 accumulator that register i of lane half g holds.
+__device__ __forceinline__ constexpr int block_row(int i, int g) { return 8 * (i >> 2) + 4 * g + (i & 3); }
+
+template <typename T, int DH, int ROWS>
+struct Tile {
+  static constexpr int kRowBytes = DH * static_cast<int>(sizeof(T)), kPieces = kRowBytes / 16, kBytes = ROWS * kRowBytes;
+  static constexpr int kPerPiece = 16 / static_cast<int>(sizeof(T));
+  static_assert(DH % 32 == 0 && ROWS % 16 == 0);
+  // Which piece sits in slot s of row r: s ^ swizzle(r).  Eight consecutive rows read at one column (row_fragment) and four
+  // rows at two neighbouring pieces (what sixteen lanes read in column_fragment) fall on different banks.
+  __device__ static constexpr int swizzle(int r) {
+    return kPieces >= 8 ? ((r & 3) << 1) | ((r >> 2) & 1) : (((r >> 1) & 1) << 1) | ((r >> 2) & 1);
+  }
+  __device__ static Fragment<T> row_fragment(const unsigned char* tile, int r0, int kk, int lane) {
+    const int n = lane & 31, g = lane >> 5, s = swizzle(n);
+    const unsigned char* row = tile + (r0 + n) * kRowBytes;
+    if constexpr (sizeof(T) == 2) {
+      return *reinterpret_cast<const bf16x8*>(row + ((2 * kk + g) ^ s) * 16);
+    } else {
+      const f32x4 lo = *reinterpret_cast<const f32x4*>(row + ((4 * kk + 2 * g) ^ s) * 16);
+      const f32x4 hi = *reinterpret_cast<const f32x4*>(row + ((4 * kk + 2 * g + 1) ^ s) * 16);
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+  }
+  // r0 a multiple of 16, c0 of 32
+  __device__ static Fragment<T> column_fragment(const unsigned char* tile, int r0, int c0, int lane) {
+    if constexpr (sizeof(T) == 2) {
+      // ds_read_b64_tr_b16: each lane of a group of 16 gets a column of the 4 x 16 block whose rows the group's lanes point
+      // at, four lanes a row
+      const int r = 4 * (lane >> 5) + (lane & 15) / 4, piece = c0 / 8 + 2 * ((lane >> 4) & 1) + (lane & 3) / 2;
+      const unsigned char* p = tile + (r0 + r) * kRowBytes + (piece ^ swizzle(r)) * 16 + (lane & 1) * 8;
+      // (eight rows on, the swizzle is the same)
+      const bf16x4 lo = transposed(p), hi = transposed(p + 8 * kRowBytes);
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      const int n = lane & 31, g = lane >> 5, piece = (c0 + n) / 4, in = n & 3;
+      f32x8 v;
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const int r = chain_k(g, t);
+        v[t] = *reinterpret_cast<const float*>(tile + (r0 + r) * kRowBytes + (piece ^ swizzle(r)) * 16 + in * 4);
+      }
+      return v;
+    }
+  }
+
+ private:
+  __device__ static bf16x4 transposed(const unsigned char* q) {
+    return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(q)));
+  }
+};
+
+// Rows of a strided row-major matrix, `width` elements each: what a tile is filled from.
+struct Rows {
+  const void* base;   // the first row, at this head's first column; uniform over the workgroup
+  unsigned stride;    // bytes from row to row, at least the width, below 2^24
+  unsigned width;     // bytes of a row
+  bool pieces;        // base, stride and width are multiples of 16 bytes
+};
+
+// Fills tiles by WAVES waves, 1 KiB a load, from memory straight to LDS.  Rows at or past the given count and columns past the
+// width come out as zeros: the loads go through a buffer whose size ends with the last row, and what lies outside reads as zero.
+template <typename T, int DH, int ROWS, int WAVES>
+struct TileLoader {
+  using Shape = Tile<T, DH, ROWS>;
+  static constexpr int kLoads = Shape::kBytes / 1024 / WAVES;  // a wave's, for one tile
+  static_assert(kLoads * WAVES * 1024 == Shape::kBytes && ROWS <= 128);
+  unsigned offset[kLoads];
+
+  __device__ void init(const Rows& m, int tid) {
+    const int lane = tid & 63, wave = tid >> 6;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int at = (wave + WAVES * i) * 64 + lane, row = at / Shape::kPieces, piece = (at % Shape::kPieces) ^ Shape::swizzle(row);
+      offset[i] = piece * 16u < m.width ? row * m.stride + piece * 16u : 0x80000000u;
+    }
+  }
+  // Asks for rows row0 .. row0 + ROWS - 1, those at or past `rows` as zeros.  kLoads loads a wave (none where rows are not
+  // made of whole pieces: then the tile is copied here and now, element by element).
+  __device__ void issue(const Rows& m, int row0, int rows, unsigned char* tile, int tid) const {
+    const char* first = static_cast<const char*>(m.base) + static_cast<int64_t>(row0) * m.stride;
+    const int count = min(rows - row0, ROWS);
+    if (m.pieces) {
+      const uint64_t at = reinterpret_cast<uint64_t>(first);
+      const unsigned size = count > 0 ? (count - 1) * m.stride + m.width : 0;
+      u32x4 resource;
+      resource[0] = __builtin_amdgcn_readfirstlane(static_cast<unsigned>(at));
+      resource[1] = __builtin_amdgcn_readfirstlane(static_cast<unsigned>(at >> 32) & 0xffffu);
+      resource[2] = __builtin_amdgcn_readfirstlane(size);
+      resource[3] = 0x00020000u;
+      const unsigned lds = __builtin_amdgcn_readfirstlane(lds_offset_of(tile) + (tid >> 6) * 1024);
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                     : : "s"(lds + WAVES * 1024 * i), "v"(offset[i]), "s"(resource) : "memory");
+    } else {
+      const unsigned columns = m.width / sizeof(T);
+      for (unsigned i = tid; i < ROWS * DH; i += WAVES * 64) {
+        const int r = i / DH, c = i % DH;
+        T v{};
+        if (r < count && c < static_cast<int>(columns)) v = *reinterpret_cast<const T*>(first + r * static_cast<int64_t>(m.stride) + c * sizeof(T));
+        *reinterpret_cast<T*>(tile + r * Shape::kRowBytes + ((c / Shape::kPerPiece) ^ Shape::swizzle(r)) * 16 + c % Shape::kPerPiece * sizeof(T)) = v;
+      }
+    }
+  }
+};
+
+// 64 words, those from `count` on as zeros, straight to LDS: one load of one wave.
+__device__ __forceinline__ void words_to_lds(const void* from, int count, void* to, int lane) {
+  const uint64_t at = reinterpret_cast<uint64_t>(from);
+  u32x4 resource;
+  resource[0] = __builtin_amdgcn_readfirstlane(static_cast<unsigned>(at));
+  resource[1] = __builtin_amdgcn_readfirstlane(static_cast<unsigned>(at >> 32) & 0xffffu);
+  resource[2] = __builtin_amdgcn_readfirstlane(count * 4u);
+  resource[3] = 0x00020000u;
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+               : : "s"(__builtin_amdgcn_readfirstlane(lds_offset_of(to))), "v"(lane * 4u), "s"(resource) : "memory");
+}
+
+// The 16-deep fragments of one row of `width` bytes, straight from memory: lane half g's slots hold columns 16 kk + 8g .. + 7.
+// A row that is not live, and columns past the width, are zeros.
+template <typename T, int DH>
+__device__ __forceinline__ void load_row(const void* row, unsigned width, bool pieces, bool live, int g, Fragment<T> (&f)[DH / 16]) {
+#pragma unroll
+  for (int kk = 0; kk < DH / 16; ++kk) {
+    const int c = 16 * kk + 8 * g;
+    Fragment<T> v;
+#pragma unroll
+    for (int t = 0; t < 8; ++t) v[t] = 0;
+    const T* p = static_cast<const T*>(row) + c;
+    if (pieces) {
+      if constexpr (sizeof(T) == 2) {
+        if (live && c * 2u < width) v = *reinterpret_cast<const bf16x8*>(p);
+      } else {
+        f32x4 lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
+        if (live && c * 4u < width) lo = *reinterpret_cast<const f32x4*>(p);
+        if (live && (c + 4) * 4u < width) hi = *reinterpret_cast<const f32x4*>(p + 4);
+        v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      }
+    } else if (live) {
+#pragma unroll
+      for (int t = 0; t < 8; ++t)
+        if ((c + t) * sizeof(T) < width) {
+          if constexpr (sizeof(T) == 2) v[t] = __builtin_bit_cast(__bf16, p[t].bits);
+          else v[t] = p[t];
+        }
+    }
+    f[kk] = v;
+  }
+}
+
+// A transposed accumulator block (lane n = row, registers = columns block_row(i, g)) into that row, scaled; columns from `width`
+// (elements) on are left out.  `quads`: four neighbouring elements may be stored at once.
+template <typename T>
+__device__ __forceinline__ void store_block(T* row, const f32x16& d, float factor, int c0, int width, bool quads, int g) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int c = c0 + 8 * j + 4 * g;
+    if (quads) {
+      if (c >= width) continue;
+      if constexpr (sizeof(T) == 2) {
+        bf16x4 v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = static_cast<__bf16>(d[4 * j + r] * factor);
+        *reinterpret_cast<bf16x4*>(row + c) = v;
+      } else {
+        *reinterpret_cast<f32x4*>(row + c) = f32x4{d[4 * j] * factor, d[4 * j + 1] * factor, d[4 * j + 2] * factor, d[4 * j + 3] * factor};
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (c + r < width) store_as(row + c + r, d[4 * j + r] * factor);
+    }
+  }
+}
+
+}  // namespace lime
