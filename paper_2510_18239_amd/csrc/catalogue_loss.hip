@@ -8,7 +8,7 @@
 #include <algorithm>
 
 #include "encoder.hpp"
-#include "tiles.hpp"
+#include "fold.hpp"
 
 namespace lime {
 namespace {
@@ -34,18 +34,19 @@ struct Args {
   int splits, chunk;
 };
 
-constexpr int kGatherRows = 64;  // the fewest rows a workgroup of the gather takes
+constexpr int kGatherRows = 64;  // rows a workgroup of the gather takes at a time
 
 // Lists the rows with a target.  Every workgroup counts all targets by itself (they are few next to the products), so that no
 // workgroup waits for another.
 template <typename T, bool BACKWARD>
 __global__ __launch_bounds__(256) void gather_kernel(Args a, int64_t each) {
   __shared__ int sums[4][2];
-  __shared__ int place[256];
+  __shared__ int place[kGatherRows];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t begin = blockIdx.x * each, end = min(begin + each, a.rows);
   auto has = [&](int64_t i) { return static_cast<unsigned>(a.targets[i]) < static_cast<unsigned>(a.items); };
   int before = 0, all = 0;
+#pragma unroll 8
   for (int64_t i = tid; i < a.rows; i += 256) {
     const int x = has(i);
     all += x, before += i < begin ? x : 0;
@@ -56,31 +57,46 @@ __global__ __launch_bounds__(256) void gather_kernel(Args a, int64_t each) {
   before = sums[0][0] + sums[1][0] + sums[2][0] + sums[3][0], all = sums[0][1] + sums[1][1] + sums[2][1] + sums[3][1];
   if (blockIdx.x == 0 && tid == 0) a.live[0] = all;
   const bool whole = all == a.rows;
-  for (int64_t at = begin; at < end; at += 256) {
-    const int64_t i = at + tid;
-    const bool x = i < end && has(i);
-    const unsigned long long votes = __ballot(x);
-    __syncthreads();
-    if (lane == 0) sums[wave][0] = __popcll(votes);
-    __syncthreads();
-    int to = before + __popcll(votes & ((1ull << lane) - 1));
-    for (int w = 0; w < wave; ++w) to += sums[w][0];
-    before += sums[0][0] + sums[1][0] + sums[2][0] + sums[3][0];
-    place[tid] = x ? to : -1;
-    if (x) {
-      a.live[1 + to] = static_cast<int>(i);
-      if constexpr (BACKWARD) a.c_lse2[to] = a.lse[i] * kLog2e, a.c_g[to] = a.dloss[i] * a.scale, a.c_target[to] = a.targets[i];
-    } else if (i < end) {
-      if constexpr (!BACKWARD) a.loss[i] = 0.f, a.lse[i] = 0.f;
+  for (int64_t at = begin; at < end; at += kGatherRows) {
+    if (wave == 0) {  // 64 rows' places
+      const int64_t i = at + lane;
+      const bool x = i < end && has(i);
+      const unsigned long long votes = __ballot(x);
+      const int to = before + __popcll(votes & ((1ull << lane) - 1));
+      before += __popcll(votes);
+      place[lane] = x ? to : -1;
+      if (x) {
+        a.live[1 + to] = static_cast<int>(i);
+        if constexpr (BACKWARD) a.c_lse2[to] = a.lse[i] * kLog2e, a.c_g[to] = a.dloss[i] * a.scale, a.c_target[to] = a.targets[i];
+      } else if (i < end) {
+        if constexpr (!BACKWARD) a.loss[i] = 0.f, a.lse[i] = 0.f;
+      }
     }
     if (whole) continue;
     __syncthreads();
-    const int64_t here = min<int64_t>(256, end - at) * a.d;
-    for (int64_t e = tid; e < here; e += 256) {
-      const int r = static_cast<int>(e / a.d), c = static_cast<int>(e % a.d);
-      if (place[r] >= 0) static_cast<T*>(a.packed)[static_cast<int64_t>(place[r]) * a.d + c] = static_cast<const T*>(a.x)[(at + r) * a.d + c];
-      else if (BACKWARD && a.dx) store_as(static_cast<T*>(a.dx) + (at + r) * a.d + c, 0.f);
+    const int here = static_cast<int>(min<int64_t>(kGatherRows, end - at));
+#pragma unroll 4
+    for (int r = wave; r < here; r += 4) {  // a wave a row
+      const T* from = static_cast<const T*>(a.x) + (at + r) * a.d;
+      const int to = place[r];
+      T* dst = to >= 0 ? static_cast<T*>(a.packed) + static_cast<int64_t>(to) * a.d : static_cast<T*>(a.dx) + (at + r) * a.d;
+      if (to < 0 && (!BACKWARD || a.dx == nullptr)) continue;
+      if (a.x_pieces && a.quads) {  // rows of whole 16-byte pieces: at most 64 of them
+        const int c = lane * static_cast<int>(16 / sizeof(T));
+        if (c < a.d) {
+          u32x4 v = {0, 0, 0, 0};
+          if (to >= 0) v = *reinterpret_cast<const u32x4*>(from + c);
+          *reinterpret_cast<u32x4*>(dst + c) = v;
+        }
+      } else {
+        for (int c = lane; c < a.d; c += 64) {
+          T v{};
+          if (to >= 0) v = from[c];
+          dst[c] = v;
+        }
+      }
     }
+    __syncthreads();
   }
 }
 
@@ -240,24 +256,20 @@ __global__ __launch_bounds__(256) void catalogue_dx_kernel(Args a) {
   for (int ob = 0; ob < OB; ++ob) store_block(to, dx[ob], 1.f, 32 * ob, D, true, g);
 }
 
-// dX_i = dloss_i scale (the chunks' sums - W_target), D / 4 lanes a row.
+// dX_i = dloss_i scale (the chunks' sums - W_target).
 template <typename T, int D>
-__global__ __launch_bounds__(256) void catalogue_dx_fold_kernel(Args a) {
-  constexpr int LANES = D / 4;
-  const int row = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, c = threadIdx.x % LANES * 4, count = a.live[0];
-  if (row >= count || c >= a.d) return;
-  f32x4 sum = {0, 0, 0, 0};
-  for (int s = 0; s < a.splits; ++s) {
-    const f32x4 p = *reinterpret_cast<const f32x4*>(a.parts + (static_cast<int64_t>(s) * a.rows + row) * D + c);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) sum[j] += p[j];
-  }
+__global__ __launch_bounds__(256) void catalogue_dx_fold_kernel(Args a, int groups) {
+  const Folder<D> at(groups);
+  const int row = blockIdx.x * at.rows + at.row, c = 4 * at.t;
+  const bool live = row < a.live[0];
+  f32x4 sum = at.sum(a.parts + static_cast<int64_t>(row) * D, a.rows * D, a.splits, groups, live);
+  if (!live || at.group != 0) return;
   const T* w = static_cast<const T*>(a.w) + static_cast<int64_t>(a.c_target[row]) * a.d + c;
-  T* to = static_cast<T*>(a.dx) + static_cast<int64_t>(a.live[1 + row]) * a.d + c;
   const float f = a.c_g[row];
 #pragma unroll
   for (int j = 0; j < 4; ++j)
-    if (c + j < a.d) store_as(to + j, f * (sum[j] - to_float(w[j])));
+    if (c + j < a.d) sum[j] = f * (sum[j] - to_float(w[j]));
+  store_four(static_cast<T*>(a.dx) + static_cast<int64_t>(a.live[1 + row]) * a.d, sum, c, a.d, a.quads);
 }
 
 // sum_i e_iv X_i over a chunk of the listed rows, 32 items a wave.
@@ -350,21 +362,12 @@ __global__ __launch_bounds__(256) void catalogue_dw_kernel(Args a) {
 }
 
 template <typename T, int D>
-__global__ __launch_bounds__(256) void catalogue_dw_fold_kernel(Args a) {
-  constexpr int LANES = D / 4;
-  const int64_t item = static_cast<int64_t>(blockIdx.x) * (256 / LANES) + threadIdx.x / LANES;
-  const int c = threadIdx.x % LANES * 4;
-  if (item >= a.items || c >= a.d) return;
-  f32x4 sum = {0, 0, 0, 0};
-  for (int s = 0; s < a.splits; ++s) {
-    const f32x4 p = *reinterpret_cast<const f32x4*>(a.parts + (static_cast<int64_t>(s) * a.items + item) * D + c);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) sum[j] += p[j];
-  }
-  T* to = static_cast<T*>(a.dw) + item * a.d + c;
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (c + j < a.d) store_as(to + j, sum[j]);
+__global__ __launch_bounds__(256) void catalogue_dw_fold_kernel(Args a, int groups) {
+  const Folder<D> at(groups);
+  const int64_t item = static_cast<int64_t>(blockIdx.x) * at.rows + at.row;
+  const bool live = item < a.items;
+  const f32x4 sum = at.sum(a.parts + item * D, static_cast<int64_t>(a.items) * D, a.splits, groups, live);
+  if (live && at.group == 0) store_four(static_cast<T*>(a.dw) + item * a.d, sum, 4 * at.t, a.d, a.quads);
 }
 
 int padded(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
@@ -409,7 +412,7 @@ Args args_of(const CatalogueLoss& x, const Plan& p, void* workspace) {
   a.x = x.X, a.w = x.W, a.targets = x.targets, a.loss = x.loss, a.lse = x.lse, a.dloss = x.dloss, a.dx = x.dX, a.dw = x.dW;
   a.rows = x.rows, a.items = x.items, a.d = x.d, a.scale = x.scale;
   a.x_pieces = multiple(x.X, 16) && x.d * e % 16 == 0, a.w_pieces = multiple(x.W, 16) && x.d * e % 16 == 0;
-  a.quads = x.d % 4 == 0 && multiple(x.dW, 4 * e);
+  a.quads = x.d % 4 == 0 && multiple(x.dW, 16) && multiple(x.dX, 16);
   char* at = static_cast<char*>(workspace);
   a.live = reinterpret_cast<int32_t*>(at), at += p.live;
   a.packed = at, at += p.packed;
@@ -447,13 +450,14 @@ hipError_t forward(Args a, const Plan& p, hipStream_t s) {
 
 template <typename T, int D>
 hipError_t backward(Args a, const Plan& p, hipStream_t s) {
-  constexpr int STEP = sizeof(T) == 2 ? 64 : 32, PER = 256 / (D / 4);
+  constexpr int STEP = sizeof(T) == 2 ? 64 : 32;
   if (hipError_t e = gather<T, true>(a, s); e != hipSuccess) return e;
   if (a.dx) {
     static PerDevice granted;
     a.splits = p.rows.splits, a.chunk = p.rows.chunk;
     if (hipError_t e = launch(granted, catalogue_dx_kernel<T, D, STEP>, (a.rows + 127) / 128 * a.splits, 2 * Tile<T, D, STEP>::kBytes, a, s); e != hipSuccess) return e;
-    hipLaunchKernelGGL((catalogue_dx_fold_kernel<T, D>), dim3(static_cast<unsigned>((a.rows + PER - 1) / PER)), dim3(256), 0, s, a);
+    const int groups = fold_groups(a.splits, D / 4), per = 256 / (D / 4) / groups;
+    hipLaunchKernelGGL((catalogue_dx_fold_kernel<T, D>), dim3(static_cast<unsigned>((a.rows + per - 1) / per)), dim3(256), 0, s, a, groups);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
   if (a.dw) {
@@ -462,7 +466,8 @@ hipError_t backward(Args a, const Plan& p, hipStream_t s) {
     const int64_t tiles = (static_cast<int64_t>(a.items) + 127) / 128;
     if (hipError_t e = launch(granted, catalogue_dw_kernel<T, D, STEP>, tiles * a.splits, 2 * (Tile<T, D, STEP>::kBytes + 1024), a, s); e != hipSuccess) return e;
     if (a.splits > 1) {
-      hipLaunchKernelGGL((catalogue_dw_fold_kernel<T, D>), dim3(static_cast<unsigned>((static_cast<int64_t>(a.items) + PER - 1) / PER)), dim3(256), 0, s, a);
+      const int groups = fold_groups(a.splits, D / 4), per = 256 / (D / 4) / groups;
+      hipLaunchKernelGGL((catalogue_dw_fold_kernel<T, D>), dim3(static_cast<unsigned>((static_cast<int64_t>(a.items) + per - 1) / per)), dim3(256), 0, s, a, groups);
       if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
   }

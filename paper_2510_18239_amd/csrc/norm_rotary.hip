@@ -16,7 +16,7 @@
 namespace lime {
 namespace {
 
-constexpr int kRows = 8;         // rows of a workgroup's turn
+constexpr int kRows = 8, kBackRows = 32;  // rows of a workgroup's turn, forward and backward
 constexpr int kMaxGroups = 1024; // workgroups of a backward pass: each leaves one partial sum of the weights' gradients
 constexpr int kMaxHalf = kMaxRotaryHead / 2;
 
@@ -31,7 +31,7 @@ struct Args {
   int64_t rows;
   int dh, lanes;    // lanes of a head, a power of two
   float eps;
-  float* partial;   // [groups][2][dh]
+  float* partial;   // [2][dh][groups]
   double turns[kMaxHalf];  // base^(-2 i / dh) / (2 pi)
 };
 
@@ -69,14 +69,14 @@ __device__ __forceinline__ float lanes_sum(float x, int lanes) {
 }
 
 // A lane's part of a head: PARTS pieces of VEC elements of the first half, and their partners.
-template <typename T, int VEC, int PARTS, bool BACKWARD>
+template <typename T, int VEC, int PARTS, bool BACKWARD, int ROWS>
 __global__ __launch_bounds__(256) void norm_rotary_kernel(Args a) {
-  __shared__ float2 turned[kRows][kMaxHalf];  // cosine, sine
-  __shared__ float sums[BACKWARD ? 256 : 1];
+  __shared__ float2 turned[ROWS][kMaxHalf];  // cosine, sine
+  __shared__ float sums[BACKWARD ? 4 : 1][2][kMaxRotaryHead];  // of the waves
   const int tid = threadIdx.x, half = a.dh / 2, t = tid % a.lanes, unit = tid / a.lanes, units = 256 / a.lanes;
   float dgamma[BACKWARD ? 2 : 1][2][PARTS][VEC] = {};  // side, half
-  for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * kRows; row0 < a.rows; row0 += static_cast<int64_t>(gridDim.x) * kRows) {
-    const int count = static_cast<int>(min<int64_t>(kRows, a.rows - row0));
+  for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * ROWS; row0 < a.rows; row0 += static_cast<int64_t>(gridDim.x) * ROWS) {
+    const int count = static_cast<int>(min<int64_t>(ROWS, a.rows - row0));
     __syncthreads();  // everyone is done with the last rows' angles
     for (int i = tid; i < count * half; i += 256) {
       const int r = i / half, c = i % half;
@@ -154,7 +154,8 @@ __global__ __launch_bounds__(256) void norm_rotary_kernel(Args a) {
       }
     }
   }
-  if constexpr (BACKWARD) {  // the workgroup's sums, its units in ascending order
+  if constexpr (BACKWARD) {  // the workgroup's sums: a wave's lanes that hold the same elements, then the four waves
+    const int lane = tid & 63, wave = tid >> 6;
 #pragma unroll
     for (int side = 0; side < 2; ++side)
 #pragma unroll
@@ -163,16 +164,16 @@ __global__ __launch_bounds__(256) void norm_rotary_kernel(Args a) {
         for (int p = 0; p < PARTS; ++p)
 #pragma unroll
           for (int i = 0; i < VEC; ++i) {
-            __syncthreads();
-            sums[tid] = dgamma[side][h][p][i];
-            __syncthreads();
+            float x = dgamma[side][h][p][i];
+            for (int o = a.lanes; o < 64; o *= 2) x += __shfl_xor(x, o, 64);
             const int c = (t + p * a.lanes) * VEC + i;
-            if (unit == 0 && c < half) {
-              float total = 0.f;
-              for (int u = 0; u < units; ++u) total += sums[u * a.lanes + t];
-              a.partial[(static_cast<int64_t>(blockIdx.x) * 2 + side) * a.dh + h * half + c] = total;
-            }
+            if (lane < a.lanes && c < half) sums[wave][side][h * half + c] = x;
           }
+    __syncthreads();
+    for (int i = tid; i < 2 * a.dh; i += 256) {
+      const int side = i / a.dh, c = i % a.dh;
+      a.partial[static_cast<int64_t>(i) * gridDim.x + blockIdx.x] = sums[0][side][c] + sums[1][side][c] + sums[2][side][c] + sums[3][side][c];
+    }
   }
 }
 
@@ -183,19 +184,19 @@ __global__ __launch_bounds__(256) void norm_rotary_fold_kernel(const float* part
   if (side > 1) return;
   T* to = side ? dk : dq;
   float total = 0.f;
-  for (int i = lane; i < groups; i += 64) total += partial[(static_cast<int64_t>(i) * 2 + side) * dh + c];
+  for (int i = lane; i < groups; i += 64) total += partial[static_cast<int64_t>(at) * groups + i];
   total = wave_sum(total);
   if (to && lane == 0) store_as(to + c, total);
 }
 
 bool multiple(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
-int64_t groups_of(int64_t rows) { return std::min<int64_t>(kMaxGroups, (rows + kRows - 1) / kRows); }
+int64_t groups_of(int64_t rows) { return std::min<int64_t>(kMaxGroups, (rows + kBackRows - 1) / kBackRows); }
 
 template <typename T, int VEC, int PARTS>
 hipError_t launch(const Args& a, bool backward, hipStream_t s) {
   const int64_t groups = backward ? groups_of(a.rows) : (a.rows + kRows - 1) / kRows;
-  if (backward) hipLaunchKernelGGL((norm_rotary_kernel<T, VEC, PARTS, true>), dim3(static_cast<unsigned>(groups)), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((norm_rotary_kernel<T, VEC, PARTS, false>), dim3(static_cast<unsigned>(groups)), dim3(256), 0, s, a);
+  if (backward) hipLaunchKernelGGL((norm_rotary_kernel<T, VEC, PARTS, true, kBackRows>), dim3(static_cast<unsigned>(groups)), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((norm_rotary_kernel<T, VEC, PARTS, false, kRows>), dim3(static_cast<unsigned>(groups)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

@@ -6,6 +6,7 @@
 // key head, in memory order: a tile of keys and values is read once for a whole group, in a prompt as for a single query.
 #include <algorithm>
 
+#include "fold.hpp"
 #include "sequences.hpp"
 
 namespace lime {
@@ -152,34 +153,49 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_kernel(Args a) 
   if (a.lse != nullptr && g == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// The chunks' states of a row folded in ascending order; DH / 4 lanes a row.
+// The chunks' states of a row folded (see fold.hpp).
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void sequence_attention_merge_kernel(Args a) {
-  constexpr int LANES = DH / 4, PER = 256 / LANES;
-  const int tid = threadIdx.x, t = tid % LANES, pairs = a.B * a.hk;
-  const int pair = blockIdx.x % pairs, b = pair / a.hk, kv = pair % a.hk;
-  const int r = blockIdx.x / pairs * PER + tid / LANES;
+__global__ __launch_bounds__(256) void sequence_attention_merge_kernel(Args a, int groups) {
+  __shared__ f32x4 met[256];
+  __shared__ float met_m[256], met_l[256];
+  const Folder<DH> at(groups);
+  const int pairs = a.B * a.hk, pair = blockIdx.x % pairs, b = pair / a.hk, kv = pair % a.hk;
+  const int r = static_cast<int>(blockIdx.x / pairs) * at.rows + at.row;
   const Span qs = span_of(a.q_offsets, a.q_lens, b, a.q_rows, a.max_q);
-  if (r >= qs.slot * a.group) return;
-  const int64_t each = static_cast<int64_t>(a.max_q) * a.group, step = pairs * each, at = pair * each + r;
-  float m = -INFINITY;
-  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_ml[(at + s * step) * 2]);
-  const float base = m == -INFINITY ? 0.f : m;
-  float l = 0.f;
+  const bool live = r < qs.slot * a.group;
+  const int64_t each = static_cast<int64_t>(a.max_q) * a.group, step = pairs * each, state = pair * each + r;
+  float m = -INFINITY, l = 0.f;
   f32x4 o = {0, 0, 0, 0};
-  for (int s = 0; s < a.splits; ++s) {
-    const float f = __builtin_amdgcn_exp2f(a.part_ml[(at + s * step) * 2] - base);
-    l = fmaf(f, a.part_ml[(at + s * step) * 2 + 1], l);
-    const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_o + (at + s * step) * DH + 4 * t);
+  auto add = [&](float m1, float l1, const f32x4& o1) {
+    const float to = fmaxf(m, m1), base = to == -INFINITY ? 0.f : to;
+    const float f0 = __builtin_amdgcn_exp2f(m - base), f1 = __builtin_amdgcn_exp2f(m1 - base);
+    m = to, l = l * f0 + l1 * f1;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) o[j] = fmaf(f, x[j], o[j]);
+    for (int j = 0; j < 4; ++j) o[j] = o[j] * f0 + o1[j] * f1;
+  };
+  if (live) {
+#pragma unroll 4
+    for (int s = at.group; s < a.splits; s += groups) {
+      const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (state + s * step) * 2);
+      add(ml.x, ml.y, *reinterpret_cast<const f32x4*>(a.part_o + (state + s * step) * DH + 4 * at.t));
+    }
   }
+  for (int half = groups / 2; half; half /= 2) {
+    __syncthreads();
+    met[threadIdx.x] = o, met_m[threadIdx.x] = m, met_l[threadIdx.x] = l;
+    __syncthreads();
+    if (at.group < half) {
+      const int other = threadIdx.x + half * Folder<DH>::kLanes;
+      add(met_m[other], met_l[other], met[other]);
+    }
+  }
+  if (!live || at.group != 0) return;
   const float inverse = l == 0.f ? 0.f : 1.f / l;
   const int64_t row = (qs.start + r / a.group) * a.hq + kv * a.group + r % a.group;
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (4 * t + j < a.dh) store_as(static_cast<T*>(a.o) + row * a.dh + 4 * t + j, o[j] * inverse);
-  if (a.lse != nullptr && t == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+  for (int j = 0; j < 4; ++j) o[j] *= inverse;
+  store_four(static_cast<T*>(a.o) + row * a.dh, o, 4 * at.t, a.dh, a.quads);
+  if (a.lse != nullptr && at.t == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 struct Plan {
@@ -228,8 +244,9 @@ hipError_t run(const Args& a, const Plan& p, hipStream_t s) {
   const int64_t pairs = static_cast<int64_t>(a.B) * a.hk, blocks = pairs * a.tiles * a.splits;
   hipError_t e = p.waves == 1 ? launch<T, DH, 1, KEYS, 2>(a, blocks, s) : launch<T, DH, 4, KEYS, 2>(a, blocks, s);
   if (e != hipSuccess || a.splits == 1) return e;
-  const int64_t rows = static_cast<int64_t>(a.max_q) * a.group, per = 256 / (DH / 4);
-  hipLaunchKernelGGL((sequence_attention_merge_kernel<T, DH>), dim3(static_cast<unsigned>(pairs * ((rows + per - 1) / per))), dim3(256), 0, s, a);
+  const int groups = fold_groups(a.splits, DH / 4);
+  const int64_t rows = static_cast<int64_t>(a.max_q) * a.group, per = 256 / (DH / 4) / groups;
+  hipLaunchKernelGGL((sequence_attention_merge_kernel<T, DH>), dim3(static_cast<unsigned>(pairs * ((rows + per - 1) / per))), dim3(256), 0, s, a, groups);
   return hipGetLastError();
 }
 
@@ -241,7 +258,7 @@ bool sequence_attention_fits(const SequenceAttention& a) {  // 2^32 work items a
   const int64_t rows = static_cast<int64_t>(a.max_q) * (a.hq / a.hk), pairs = static_cast<int64_t>(a.B) * a.hk;
   if (rows >= (int64_t{1} << 31) - 128 || pairs >= (int64_t{1} << 24)) return false;
   const Plan p = plan_of(a);
-  return pairs * p.tiles * p.splits < (int64_t{1} << 26) / p.waves && (p.splits == 1 || pairs * ((rows + 7) / 8) < (int64_t{1} << 24));
+  return pairs * p.tiles * p.splits < (int64_t{1} << 26) / p.waves && (p.splits == 1 || pairs * rows < (int64_t{1} << 24));
 }
 
 size_t sequence_attention_workspace(const SequenceAttention& a) { return std::max<size_t>(plan_of(a).bytes, 256); }

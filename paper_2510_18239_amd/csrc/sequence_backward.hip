@@ -4,9 +4,11 @@
 // Two kernels, each with one side's rows and sums in registers while the other side's tiles stream past, so that every sum has one
 // owner and one order (no atomics): the first holds queries (rows as in the forward pass) and also leaves D and lse, by head, for
 // the second, which holds keys.  Seven products of the tiles where a kernel that kept both sides' sums would do five: the sums of
-// the other side would have to meet in memory.  p and e are rounded to the storage type, as operands of the last products.
+// the other side would have to meet in memory.  Where the workgroups of a side are too few for the chip, the side that streams past is
+// cut into chunks whose sums a third kernel folds (fold.hpp).  p and e are rounded to the storage type, as operands of the last products.
 #include <algorithm>
 
+#include "fold.hpp"
 #include "sequences.hpp"
 
 namespace lime {
@@ -20,7 +22,9 @@ struct Args {
   float *lse2, *delta;  // [hq][q_rows]: lse log2 e, D
   void *dq, *dk, *dv;
   int64_t q_rows, k_rows;
+  float *part_q, *part_kv;  // chunks > 1: [q_splits][q_rows][hq][padded dh], [k_splits][2][k_rows][hk][padded dh]
   int B, max_q, max_k, hq, hk, group, dh, tiles;
+  int q_splits, q_chunk, k_splits, k_chunk;  // chunks of keys (in keys), and of the steps over queries
   float scale;
   bool pieces, causal, quads;
 };
@@ -32,7 +36,8 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
   constexpr int KB = KEYS / 32, OB = DH / 32, NK = DH / 16, ROWS = 32 * WAVES;
   extern __shared__ __align__(1024) unsigned char smem[];  // [2][keys, values]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
-  const int pairs = a.B * a.hk, pair = blockIdx.x % pairs, tile = a.tiles - 1 - static_cast<int>(blockIdx.x) / pairs;
+  const int pairs = a.B * a.hk, pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
+  const int split = rest % a.q_splits, tile = a.tiles - 1 - rest / a.q_splits;
   const int b = pair / a.hk, kv = pair % a.hk;
   const Span qs = span_of(a.q_offsets, a.q_lens, b, a.q_rows, a.max_q), ks = span_of(a.k_offsets, a.k_lens, b, a.k_rows, a.max_k);
   const int r0 = tile * ROWS, slot_rows = qs.slot * a.group, used_rows = qs.used * a.group;
@@ -43,22 +48,23 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
   auto last_limit = [&](int rows_end) { return rows_end > 0 ? keys_seen((rows_end - 1) / a.group, qs.used, ks.used, a.causal) : 0; };
   const int w0 = r0 + 32 * wave, wave_most = w0 < used_rows ? last_limit(min(w0 + 32, used_rows)) : 0;
   const int wave_least = w0 + 32 <= used_rows ? keys_seen(w0 / a.group, qs.used, ks.used, a.causal) : 0;
-  const int most = r0 < used_rows ? last_limit(min(r0 + ROWS, used_rows)) : 0, steps = (most + KEYS - 1) / KEYS;
+  const int most = r0 < used_rows ? last_limit(min(r0 + ROWS, used_rows)) : 0;
+  const int k_begin = split * a.q_chunk, k_end = min(most, k_begin + a.q_chunk), steps = k_end > k_begin ? (k_end - k_begin + KEYS - 1) / KEYS : 0;
 
   const unsigned width = a.dh * sizeof(T);
-  const Rows km{static_cast<const T*>(a.k) + ks.start * a.k_stride + kv * a.dh, static_cast<unsigned>(a.k_stride * sizeof(T)), width, a.pieces};
-  const Rows vm{static_cast<const T*>(a.v) + ks.start * a.v_stride + kv * a.dh, static_cast<unsigned>(a.v_stride * sizeof(T)), width, a.pieces};
+  const Rows km{static_cast<const T*>(a.k) + (ks.start + k_begin) * a.k_stride + kv * a.dh, static_cast<unsigned>(a.k_stride * sizeof(T)), width, a.pieces};
+  const Rows vm{static_cast<const T*>(a.v) + (ks.start + k_begin) * a.v_stride + kv * a.dh, static_cast<unsigned>(a.v_stride * sizeof(T)), width, a.pieces};
   Loader kl, vl;
   kl.init(km, tid), vl.init(vm, tid);
   auto ask = [&](int i) {
     unsigned char* at = smem + i % 2 * 2 * Shape::kBytes;
-    kl.issue(km, i * KEYS, most, at, tid);
-    vl.issue(vm, i * KEYS, most, at + Shape::kBytes, tid);
+    kl.issue(km, i * KEYS, k_end - k_begin, at, tid);
+    vl.issue(vm, i * KEYS, k_end - k_begin, at + Shape::kBytes, tid);
   };
   // Few keys: all their tiles fit, and D comes from its other form, sum_j p_ij <G_i, V_j>.  <G_i, O_i> carries the rounding of O to
   // the storage type, which is as large as the difference e_ij where a row sees two keys and fades with the square root of their
   // number (two keys, bf16: gradients 5e-3 off from the rounded O, 2.6e-3 this way; past 128 keys the two are alike).
-  const bool resident = sizeof(T) == 2 && steps <= 2;
+  const bool resident = sizeof(T) == 2 && most <= 2 * KEYS;  // (and in one chunk, none is shorter)
   if (steps > 0) ask(0);
   if (resident && steps > 1) ask(1);
 
@@ -93,7 +99,7 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
       for (int t = 0; t < 8; ++t) delta = fmaf(static_cast<float>(go[kk][t]), static_cast<float>(o[kk][t]), delta);
     delta = pair_sum(delta);
   }
-  if (live && g == 0) {
+  if (live && g == 0 && split == 0) {
     const int64_t at = head * a.q_rows + qs.start + query;
     a.lse2[at] = lse2, a.delta[at] = delta;
   }
@@ -105,7 +111,7 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
     wait_lds_loads<0>();
     lds_barrier();
     if (i + 1 < steps && !resident) ask(i + 1);
-    const int key0 = i * KEYS;
+    const int key0 = k_begin + i * KEYS;
     if (key0 >= wave_most) continue;
     const unsigned char *kt = smem + i % 2 * 2 * Shape::kBytes, *vt = kt + Shape::kBytes;
     const bool partial = key0 + KEYS > wave_least;
@@ -133,6 +139,12 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
     }
   }
   if (r >= slot_rows) return;
+  if (a.q_splits > 1) {
+    float* to = a.part_q + ((split * a.q_rows + qs.start + query) * a.hq + head) * DH;
+#pragma unroll
+    for (int ob = 0; ob < OB; ++ob) store_block(to, dq[ob], 1.f, 32 * ob, DH, true, g);
+    return;
+  }
   T* out = static_cast<T*>(a.dq) + (qs.start + query) * a.dq_stride + head * a.dh;
 #pragma unroll
   for (int ob = 0; ob < OB; ++ob) store_block(out, dq[ob], a.scale, 32 * ob, a.dh, a.quads, g);
@@ -147,7 +159,7 @@ __global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
   extern __shared__ __align__(1024) unsigned char smem[];  // [2] stages
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   // first keys first: under a causal mask most queries see them
-  const int pairs = a.B * a.hk, pair = blockIdx.x % pairs, tile = blockIdx.x / pairs;
+  const int pairs = a.B * a.hk, pair = blockIdx.x % pairs, rest = blockIdx.x / pairs, split = rest % a.k_splits, tile = rest / a.k_splits;
   const int b = pair / a.hk, kv = pair % a.hk;
   const Span qs = span_of(a.q_offsets, a.q_lens, b, a.q_rows, a.max_q), ks = span_of(a.k_offsets, a.k_lens, b, a.k_rows, a.max_k);
   const int j0 = tile * KEYS;
@@ -159,7 +171,8 @@ __global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
   const int w0 = j0 + 32 * wave, wave_first = w0 < ks.used ? (a.causal ? max(0, w0 - shift) : 0) : qs.used;
   const int wave_all = w0 + 32 <= ks.used ? (a.causal ? max(0, w0 + 31 - shift) : 0) : qs.used;
   const int begin = (a.causal ? max(0, j0 - shift) : 0) / STEP * STEP;
-  const int each = j0 < ks.used && begin < qs.used ? (qs.used - begin + STEP - 1) / STEP : 0, steps = each * a.group;
+  const int each = j0 < ks.used && begin < qs.used ? (qs.used - begin + STEP - 1) / STEP : 0, all = each * a.group;
+  const int begin_step = min(all, split * a.k_chunk), steps = min(all - begin_step, a.k_chunk);
 
   const unsigned width = a.dh * sizeof(T);
   Rows qm{static_cast<const T*>(a.q) + (qs.start + begin) * a.q_stride + kv * a.group * a.dh, static_cast<unsigned>(a.q_stride * sizeof(T)), width, a.pieces};
@@ -167,15 +180,16 @@ __global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
   Loader ql, gl;
   ql.init(qm, tid), gl.init(gm, tid);
   // steps are asked for one head after the other
-  int ask_head = 0, ask_at = 0;
+  int ask_head = each ? begin_step / each : 0, ask_at = each ? begin_step % each * STEP : 0, at = ask_at;  // at: this step's first query, from `begin`
+  qm.base = static_cast<const char*>(qm.base) + ask_head * width, gm.base = static_cast<const char*>(gm.base) + ask_head * width;
   auto ask = [&](int i) {
-    unsigned char* at = smem + i % 2 * kStage;
+    unsigned char* to = smem + i % 2 * kStage;
     const int count = qs.used - begin - ask_at;
-    ql.issue(qm, ask_at, qs.used - begin, at, tid);
-    gl.issue(gm, ask_at, qs.used - begin, at + Shape::kBytes, tid);
+    ql.issue(qm, ask_at, qs.used - begin, to, tid);
+    gl.issue(gm, ask_at, qs.used - begin, to + Shape::kBytes, tid);
     if (wave < 2) {
       const float* from = (wave == 0 ? a.lse2 : a.delta) + (kv * a.group + ask_head) * a.q_rows + qs.start + begin + ask_at;
-      words_to_lds(from, min(count, STEP), reinterpret_cast<float*>(at + 2 * Shape::kBytes) + 64 * wave, lane);
+      words_to_lds(from, min(count, STEP), reinterpret_cast<float*>(to + 2 * Shape::kBytes) + 64 * wave, lane);
     }
     ask_at += STEP;
     if (ask_at >= each * STEP) {
@@ -193,7 +207,6 @@ __global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
 #pragma unroll
   for (int ob = 0; ob < OB; ++ob) dk[ob] = dv[ob] = zero_block();
 
-  int at = 0;  // this step's first query, from `begin`
   for (int i = 0; i < steps; ++i) {
     wait_lds_loads<0>();
     lds_barrier();
@@ -240,6 +253,13 @@ __global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
     }
   }
   if (key >= ks.slot) return;
+  if (a.k_splits > 1) {
+    const int64_t plane = a.k_rows * a.hk * DH;
+    float* to = a.part_kv + 2 * split * plane + ((ks.start + key) * a.hk + kv) * DH;
+#pragma unroll
+    for (int ob = 0; ob < OB; ++ob) store_block(to, dk[ob], 1.f, 32 * ob, DH, true, g), store_block(to + plane, dv[ob], 1.f, 32 * ob, DH, true, g);
+    return;
+  }
   T* dk_row = static_cast<T*>(a.dk) + (ks.start + key) * a.dk_stride + kv * a.dh;
   T* dv_row = static_cast<T*>(a.dv) + (ks.start + key) * a.dv_stride + kv * a.dh;
 #pragma unroll
@@ -249,8 +269,63 @@ __global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
   }
 }
 
+// The chunks' sums of a row of dQ (what = 0), dK (1) or dV (2) folded.
 template <typename T, int DH>
-hipError_t run(Args a, hipStream_t s) {
+__global__ __launch_bounds__(256) void sequence_attention_fold_kernel(Args a, int what, int groups) {
+  const Folder<DH> at(groups);
+  const int heads = what == 0 ? a.hq : a.hk, users = a.B, splits = what == 0 ? a.q_splits : a.k_splits;
+  const int b = blockIdx.x % users, i = static_cast<int>(blockIdx.x / users) * at.rows + at.row;
+  const Span span = what == 0 ? span_of(a.q_offsets, a.q_lens, b, a.q_rows, a.max_q) : span_of(a.k_offsets, a.k_lens, b, a.k_rows, a.max_k);
+  const bool live = i / heads < span.slot;
+  const int64_t rows = what == 0 ? a.q_rows : a.k_rows, row = span.start + i / heads, plane = rows * heads * DH;
+  const float* p = (what == 0 ? a.part_q : a.part_kv) + (what == 2 ? plane : 0) + (row * heads + i % heads) * DH;
+  f32x4 sum = at.sum(p, what == 0 ? plane : 2 * plane, splits, groups, live);
+  if (!live || at.group != 0) return;
+  const float factor = what == 2 ? 1.f : a.scale;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) sum[j] *= factor;
+  T* to = static_cast<T*>(what == 0 ? a.dq : what == 1 ? a.dk : a.dv) + row * (what == 0 ? a.dq_stride : what == 1 ? a.dk_stride : a.dv_stride) + i % heads * a.dh;
+  store_four(to, sum, 4 * at.t, a.dh, a.quads);
+}
+
+struct Plan {
+  int dh, q_tiles, k_tiles, q_splits, q_chunk, k_splits, k_chunk;
+  size_t stats, part_q, part_kv, bytes;
+};
+
+// Two workgroups of four waves a compute unit are wanted; no chunk is shorter than 256 keys (bf16; 128: fp32), or four steps over queries.
+Plan plan_of(const SequenceAttention& a) {
+  const int64_t group = a.hq / a.hk, pairs = static_cast<int64_t>(a.B) * a.hk, max_q = std::max(a.max_q, 1), max_k = std::max(a.max_k, 1);
+  const int64_t want = 2 * static_cast<int64_t>(compute_units()), step = a.dtype == 1 ? 64 : 32;
+  Plan p{};
+  p.dh = a.dh <= 32 ? 32 : a.dh <= 64 ? 64 : 128;
+  p.q_tiles = static_cast<int>((max_q * group + 127) / 128), p.k_tiles = static_cast<int>((max_k + 127) / 128);
+  auto cut = [&](int64_t tiles, int64_t length, int64_t least, int& splits, int& chunk) {
+    const int64_t most = std::max<int64_t>(1, (length + least - 1) / least), n = std::min(most, std::max<int64_t>(1, want / (pairs * tiles)));
+    const int64_t c = ((length + n - 1) / n + step - 1) / step * step;
+    chunk = static_cast<int>(std::min<int64_t>(c, (int64_t{1} << 31) - 1)), splits = static_cast<int>((length + c - 1) / c);
+  };
+  cut(p.q_tiles, max_k, 4 * step, p.q_splits, p.q_chunk);
+  const int64_t steps = (max_q + step - 1) / step * group;
+  cut(p.k_tiles, steps * step, 4 * step, p.k_splits, p.k_chunk);
+  p.k_chunk = static_cast<int>((p.k_chunk + step - 1) / step);
+  p.stats = align_up(static_cast<size_t>(a.q_rows) * a.hq * sizeof(float));
+  p.part_q = p.q_splits > 1 ? align_up(static_cast<size_t>(p.q_splits) * a.q_rows * a.hq * p.dh * sizeof(float)) : 0;
+  p.part_kv = p.k_splits > 1 ? align_up(static_cast<size_t>(p.k_splits) * 2 * a.k_rows * a.hk * p.dh * sizeof(float)) : 0;
+  p.bytes = std::max<size_t>(256, 2 * p.stats + p.part_q + p.part_kv);
+  return p;
+}
+
+template <typename T, int DH>
+hipError_t fold(const Args& a, int what, int most, int heads, int splits, hipStream_t s) {
+  const int groups = fold_groups(splits, DH / 4);
+  const int64_t per = 256 / (DH / 4) / groups, rows = static_cast<int64_t>(most) * heads;
+  hipLaunchKernelGGL((sequence_attention_fold_kernel<T, DH>), dim3(static_cast<unsigned>(a.B * ((rows + per - 1) / per))), dim3(256), 0, s, a, what, groups);
+  return hipGetLastError();
+}
+
+template <typename T, int DH>
+hipError_t run(Args a, const Plan& p, hipStream_t s) {
   constexpr int STEP = sizeof(T) == 2 ? 64 : 32;
   const int64_t pairs = static_cast<int64_t>(a.B) * a.hk;
   if (a.max_q > 0) {
@@ -258,17 +333,21 @@ hipError_t run(Args a, hipStream_t s) {
     static PerDevice granted;
     const auto kernel = sequence_attention_dq_kernel<T, DH, 4, STEP>;
     if (hipError_t e = allow_lds(granted, reinterpret_cast<const void*>(kernel), lds); e != hipSuccess) return e;
-    a.tiles = static_cast<int>((static_cast<int64_t>(a.max_q) * a.group + 127) / 128);
-    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(pairs * a.tiles)), dim3(256), lds, s, a);
+    a.tiles = p.q_tiles;
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(pairs * p.q_tiles * p.q_splits)), dim3(256), lds, s, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    if (p.q_splits > 1)
+      if (hipError_t e = fold<T, DH>(a, 0, a.max_q, a.hq, p.q_splits, s); e != hipSuccess) return e;
   }
   if (a.max_k == 0) return hipSuccess;
   constexpr int lds = 2 * (2 * Tile<T, DH, STEP>::kBytes + 512);
   static PerDevice granted;
   const auto kernel = sequence_attention_dkv_kernel<T, DH, STEP>;
   if (hipError_t e = allow_lds(granted, reinterpret_cast<const void*>(kernel), lds); e != hipSuccess) return e;
-  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(pairs * ((a.max_k + 127) / 128))), dim3(256), lds, s, a);
-  return hipGetLastError();
+  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(pairs * p.k_tiles * p.k_splits)), dim3(256), lds, s, a);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess || p.k_splits == 1) return e;
+  if (hipError_t e = fold<T, DH>(a, 1, a.max_k, a.hk, p.k_splits, s); e != hipSuccess) return e;
+  return fold<T, DH>(a, 2, a.max_k, a.hk, p.k_splits, s);
 }
 
 bool multiple(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
@@ -277,30 +356,37 @@ bool multiple(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) %
 
 bool sequence_attention_backward_fits(const SequenceAttention& a) {  // 2^32 work items a launch
   const int64_t rows = static_cast<int64_t>(a.max_q) * (a.hq / a.hk), pairs = static_cast<int64_t>(a.B) * a.hk;
-  return rows < (int64_t{1} << 31) - 128 && pairs < (int64_t{1} << 24) && pairs * ((rows + 127) / 128) < (int64_t{1} << 24) &&
-         pairs * ((a.max_k + 127) / 128) < (int64_t{1} << 24);
+  if (rows >= (int64_t{1} << 31) - 128 || pairs >= (int64_t{1} << 24)) return false;
+  const Plan p = plan_of(a);
+  return pairs * p.q_tiles * p.q_splits < (int64_t{1} << 24) && pairs * p.k_tiles * p.k_splits < (int64_t{1} << 24) &&
+         (p.q_splits == 1 || a.B * static_cast<int64_t>(a.max_q) * a.hq < (int64_t{1} << 24)) &&
+         (p.k_splits == 1 || a.B * static_cast<int64_t>(a.max_k) * a.hk < (int64_t{1} << 24));
 }
 
-size_t sequence_attention_backward_workspace(const SequenceAttention& a) { return std::max<size_t>(256, 2 * align_up(static_cast<size_t>(a.q_rows) * a.hq * sizeof(float))); }
+size_t sequence_attention_backward_workspace(const SequenceAttention& a) { return plan_of(a).bytes; }
 
 hipError_t sequence_attention_backward(const SequenceAttention& x, void* workspace, hipStream_t s) {
+  const Plan p = plan_of(x);
   const size_t e = x.dtype == 1 ? 2 : 4;
   Args a{};
   a.q = x.Q, a.k = x.K, a.v = x.V, a.o = x.O, a.go = x.dO, a.dq = x.dQ, a.dk = x.dK, a.dv = x.dV, a.lse = x.lse;
   a.q_stride = x.q_stride, a.k_stride = x.k_stride, a.v_stride = x.v_stride;
   a.dq_stride = x.dq_stride, a.dk_stride = x.dk_stride, a.dv_stride = x.dv_stride;
   a.q_offsets = x.q_offsets, a.q_lens = x.q_lens, a.k_offsets = x.k_offsets, a.k_lens = x.k_lens;
-  a.lse2 = static_cast<float*>(workspace);
-  a.delta = reinterpret_cast<float*>(static_cast<char*>(workspace) + align_up(static_cast<size_t>(x.q_rows) * x.hq * sizeof(float)));
+  char* at = static_cast<char*>(workspace);
+  a.lse2 = reinterpret_cast<float*>(at), at += p.stats;
+  a.delta = reinterpret_cast<float*>(at), at += p.stats;
+  a.part_q = reinterpret_cast<float*>(at), at += p.part_q;
+  a.part_kv = reinterpret_cast<float*>(at);
+  a.q_splits = p.q_splits, a.q_chunk = p.q_chunk, a.k_splits = p.k_splits, a.k_chunk = p.k_chunk;
   a.q_rows = x.q_rows, a.k_rows = x.k_rows, a.B = x.B, a.max_q = x.max_q, a.max_k = x.max_k, a.hq = x.hq, a.hk = x.hk, a.group = x.hq / x.hk, a.dh = x.dh;
   a.scale = x.scale, a.causal = x.causal != 0;
   a.pieces = multiple(x.Q, 16) && multiple(x.K, 16) && multiple(x.V, 16) && multiple(x.O, 16) && multiple(x.dO, 16) && x.dh * e % 16 == 0 &&
              x.q_stride * e % 16 == 0 && x.k_stride * e % 16 == 0 && x.v_stride * e % 16 == 0;
   a.quads = x.dh % 4 == 0 && x.dq_stride % 4 == 0 && x.dk_stride % 4 == 0 && x.dv_stride % 4 == 0 && multiple(x.dQ, 4 * e) && multiple(x.dK, 4 * e) &&
             multiple(x.dV, 4 * e);
-  const int dh = x.dh <= 32 ? 32 : x.dh <= 64 ? 64 : 128;
-  if (x.dtype == 1) return dh == 32 ? run<bf16_t, 32>(a, s) : dh == 64 ? run<bf16_t, 64>(a, s) : run<bf16_t, 128>(a, s);
-  return dh == 32 ? run<float, 32>(a, s) : dh == 64 ? run<float, 64>(a, s) : run<float, 128>(a, s);
+  if (x.dtype == 1) return p.dh == 32 ? run<bf16_t, 32>(a, p, s) : p.dh == 64 ? run<bf16_t, 64>(a, p, s) : run<bf16_t, 128>(a, p, s);
+  return p.dh == 32 ? run<float, 32>(a, p, s) : p.dh == 64 ? run<float, 64>(a, p, s) : run<float, 128>(a, p, s);
 }
 
 }  // namespace lime
