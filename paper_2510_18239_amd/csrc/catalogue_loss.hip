@@ -112,9 +112,11 @@ template <typename T, int D, int STEP>
 __global__ __launch_bounds__(256) void catalogue_lse_kernel(Args a) {
   using Shape = Tile<T, D, STEP>;
   using Loader = TileLoader<T, D, STEP, 4>;
+  using Reader = TileReader<T, D, STEP>;
   constexpr int VB = STEP / 32, NK = D / 16;
   extern __shared__ __align__(1024) unsigned char smem[];  // [2] tiles
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
+  const Reader read(lane);
   const int split = blockIdx.x % a.splits, tile = blockIdx.x / a.splits, count = a.live[0];
   if (tile * 128 >= count) return;
   const int row = tile * 128 + 32 * wave + n;
@@ -142,7 +144,7 @@ __global__ __launch_bounds__(256) void catalogue_lse_kernel(Args a) {
     for (int vb = 0; vb < VB; ++vb) {
       s[vb] = zero_block();
 #pragma unroll
-      for (int kk = 0; kk < NK; ++kk) s[vb] = mma16(Shape::row_fragment(wt, 32 * vb, kk, lane), x[kk], s[vb]);
+      for (int kk = 0; kk < NK; ++kk) s[vb] = mma16(read.row(wt, 32 * vb, kk), x[kk], s[vb]);
     }
     if (v0 + (i + 1) * STEP > v1) {
 #pragma unroll
@@ -204,12 +206,14 @@ __global__ __launch_bounds__(256) void catalogue_loss_kernel(Args a) {
 
 // sum_v p_iv W_v over a chunk of the catalogue, 32 rows a wave.
 template <typename T, int D, int STEP>
-__global__ __launch_bounds__(256) void catalogue_dx_kernel(Args a) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void catalogue_dx_kernel(Args a) {
   using Shape = Tile<T, D, STEP>;
   using Loader = TileLoader<T, D, STEP, 4>;
+  using Reader = TileReader<T, D, STEP>;
   constexpr int VB = STEP / 32, NK = D / 16, OB = D / 32;
   extern __shared__ __align__(1024) unsigned char smem[];  // [2] tiles
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
+  const Reader read(lane);
   const int split = blockIdx.x % a.splits, tile = blockIdx.x / a.splits, count = a.live[0];
   if (tile * 128 >= count) return;
   const int row = tile * 128 + 32 * wave + n;
@@ -234,7 +238,7 @@ __global__ __launch_bounds__(256) void catalogue_dx_kernel(Args a) {
     for (int vb = 0; vb < VB; ++vb) {
       f32x16 p = zero_block();
 #pragma unroll
-      for (int kk = 0; kk < NK; ++kk) p = mma16(Shape::row_fragment(wt, 32 * vb, kk, lane), x[kk], p);
+      for (int kk = 0; kk < NK; ++kk) p = mma16(read.row(wt, 32 * vb, kk), x[kk], p);
 #pragma unroll
       for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(p[e], c, -lse2));
       if (v0 + (i + 1) * STEP > v1) {  // (zero rows past the chunk: p may be infinite there)
@@ -246,7 +250,7 @@ __global__ __launch_bounds__(256) void catalogue_dx_kernel(Args a) {
       for (int f = 0; f < 2; ++f) {
         const Fragment<T> pf = half_fragment<T>(p, f);
 #pragma unroll
-        for (int ob = 0; ob < OB; ++ob) dx[ob] = mma16(Shape::column_fragment(wt, 32 * vb + 16 * f, 32 * ob, lane), pf, dx[ob]);
+        for (int ob = 0; ob < OB; ++ob) dx[ob] = mma16(read.column(wt, 32 * vb + 16 * f, 32 * ob), pf, dx[ob]);
       }
     }
   }
@@ -274,12 +278,14 @@ __global__ __launch_bounds__(256) void catalogue_dx_fold_kernel(Args a, int grou
 
 // sum_i e_iv X_i over a chunk of the listed rows, 32 items a wave.
 template <typename T, int D, int STEP>
-__global__ __launch_bounds__(256) void catalogue_dw_kernel(Args a) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void catalogue_dw_kernel(Args a) {
   using Shape = Tile<T, D, STEP>;
   using Loader = TileLoader<T, D, STEP, 4>;
+  using Reader = TileReader<T, D, STEP>;
   constexpr int RB = STEP / 32, NK = D / 16, OB = D / 32, kStage = Shape::kBytes + 1024;  // rows; lse2, dloss scale, target, each [64]
   extern __shared__ __align__(1024) unsigned char smem[];                                 // [2] stages
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
+  const Reader read(lane);
   const int split = blockIdx.x % a.splits, tile = blockIdx.x / a.splits, count = a.live[0];
   const int item0 = tile * 128 + 32 * wave, item = item0 + n;
   const int i0 = split * a.chunk, i1 = min(count, i0 + a.chunk), steps = i1 > i0 ? (i1 - i0 + STEP - 1) / STEP : 0;
@@ -314,7 +320,7 @@ __global__ __launch_bounds__(256) void catalogue_dw_kernel(Args a) {
     for (int rb = 0; rb < RB; ++rb) {
       f32x16 e = zero_block();
 #pragma unroll
-      for (int kk = 0; kk < NK; ++kk) e = mma16(Shape::row_fragment(xt, 32 * rb, kk, lane), w[kk], e);
+      for (int kk = 0; kk < NK; ++kk) e = mma16(read.row(xt, 32 * rb, kk), w[kk], e);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int at = 32 * rb + 8 * j + 4 * g;
@@ -334,7 +340,7 @@ __global__ __launch_bounds__(256) void catalogue_dw_kernel(Args a) {
       for (int f = 0; f < 2; ++f) {
         const Fragment<T> ef = half_fragment<T>(e, f);
 #pragma unroll
-        for (int ob = 0; ob < OB; ++ob) dw[ob] = mma16(Shape::column_fragment(xt, 32 * rb + 16 * f, 32 * ob, lane), ef, dw[ob]);
+        for (int ob = 0; ob < OB; ++ob) dw[ob] = mma16(read.column(xt, 32 * rb + 16 * f, 32 * ob), ef, dw[ob]);
         // A target's e is near its row's whole weight and rarely has company: what rounding took of it is added by itself.
         if (sizeof(T) == 2 && chosen) {
           Fragment<T> rest;
@@ -344,7 +350,7 @@ __global__ __launch_bounds__(256) void catalogue_dw_kernel(Args a) {
             rest[t] = static_cast<std::conditional_t<sizeof(T) == 2, __bf16, float>>(target[32 * rb + block_row(8 * f + t, g)] == item ? x - static_cast<float>(ef[t]) : 0.f);
           }
 #pragma unroll
-          for (int ob = 0; ob < OB; ++ob) dw[ob] = mma16(Shape::column_fragment(xt, 32 * rb + 16 * f, 32 * ob, lane), rest, dw[ob]);
+          for (int ob = 0; ob < OB; ++ob) dw[ob] = mma16(read.column(xt, 32 * rb + 16 * f, 32 * ob), rest, dw[ob]);
         }
       }
     }

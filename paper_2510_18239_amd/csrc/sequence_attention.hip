@@ -34,9 +34,11 @@ template <typename T, int DH, int WAVES, int KEYS, int STAGES>
 __global__ __launch_bounds__(WAVES * 64) void sequence_attention_kernel(Args a) {
   using Shape = Tile<T, DH, KEYS>;
   using Loader = TileLoader<T, DH, KEYS, WAVES>;
+  using Reader = TileReader<T, DH, KEYS>;
   constexpr int KB = KEYS / 32, OB = DH / 32, NK = DH / 16, ROWS = 32 * WAVES;
   extern __shared__ __align__(1024) unsigned char smem[];  // [STAGES][keys, values]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
+  const Reader read(lane);
   // users and key heads fastest: the workgroups of one of them, which read the same keys, land on the same XCD where their number
   // is a multiple of eight; last tiles of rows first, under a causal mask the longest
   const int pairs = a.B * a.hk, pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
@@ -97,7 +99,7 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_kernel(Args a) 
     for (int kb = 0; kb < KB; ++kb) {
       s[kb] = zero_block();
 #pragma unroll
-      for (int kk = 0; kk < NK; ++kk) s[kb] = mma16(Shape::row_fragment(kt, 32 * kb, kk, lane), q[kk], s[kb]);
+      for (int kk = 0; kk < NK; ++kk) s[kb] = mma16(read.row(kt, 32 * kb, kk), q[kk], s[kb]);
     }
     if (key0 + KEYS > wave_least) {
 #pragma unroll
@@ -132,7 +134,7 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_kernel(Args a) 
       for (int f = 0; f < 2; ++f) {
         const Fragment<T> p = half_fragment<T>(s[kb], f);
 #pragma unroll
-        for (int ob = 0; ob < OB; ++ob) o[ob] = mma16(Shape::column_fragment(vt, 32 * kb + 16 * f, 32 * ob, lane), p, o[ob]);
+        for (int ob = 0; ob < OB; ++ob) o[ob] = mma16(read.column(vt, 32 * kb + 16 * f, 32 * ob), p, o[ob]);
       }
     }
   }

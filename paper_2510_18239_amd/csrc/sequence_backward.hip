@@ -33,9 +33,11 @@ template <typename T, int DH, int WAVES, int KEYS>
 __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args a) {
   using Shape = Tile<T, DH, KEYS>;
   using Loader = TileLoader<T, DH, KEYS, WAVES>;
+  using Reader = TileReader<T, DH, KEYS>;
   constexpr int KB = KEYS / 32, OB = DH / 32, NK = DH / 16, ROWS = 32 * WAVES;
   extern __shared__ __align__(1024) unsigned char smem[];  // [2][keys, values]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
+  const Reader read(lane);
   const int pairs = a.B * a.hk, pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
   const int split = rest % a.q_splits, tile = a.tiles - 1 - rest / a.q_splits;
   const int b = pair / a.hk, kv = pair % a.hk;
@@ -82,8 +84,8 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
       f32x16 s = zero_block(), e = zero_block();
 #pragma unroll
       for (int kk = 0; kk < NK; ++kk) {
-        s = mma16(Shape::row_fragment(kt, kb % KB * 32, kk, lane), q[kk], s);
-        e = mma16(Shape::row_fragment(vt, kb % KB * 32, kk, lane), go[kk], e);
+        s = mma16(read.row(kt, kb % KB * 32, kk), q[kk], s);
+        e = mma16(read.row(vt, kb % KB * 32, kk), go[kk], e);
       }
 #pragma unroll
       for (int x = 0; x < 16; ++x)
@@ -120,8 +122,8 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
       f32x16 s = zero_block(), e = zero_block();
 #pragma unroll
       for (int kk = 0; kk < NK; ++kk) {
-        s = mma16(Shape::row_fragment(kt, 32 * kb, kk, lane), q[kk], s);
-        e = mma16(Shape::row_fragment(vt, 32 * kb, kk, lane), go[kk], e);
+        s = mma16(read.row(kt, 32 * kb, kk), q[kk], s);
+        e = mma16(read.row(vt, 32 * kb, kk), go[kk], e);
       }
 #pragma unroll
       for (int x = 0; x < 16; ++x) e[x] = __builtin_amdgcn_exp2f(fmaf(s[x], c, -lse2)) * (e[x] - delta);
@@ -134,7 +136,7 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
       for (int f = 0; f < 2; ++f) {
         const Fragment<T> ef = half_fragment<T>(e, f);
 #pragma unroll
-        for (int ob = 0; ob < OB; ++ob) dq[ob] = mma16(Shape::column_fragment(kt, 32 * kb + 16 * f, 32 * ob, lane), ef, dq[ob]);
+        for (int ob = 0; ob < OB; ++ob) dq[ob] = mma16(read.column(kt, 32 * kb + 16 * f, 32 * ob), ef, dq[ob]);
       }
     }
   }
@@ -154,10 +156,12 @@ template <typename T, int DH, int STEP>
 __global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
   using Shape = Tile<T, DH, STEP>;
   using Loader = TileLoader<T, DH, STEP, 4>;
+  using Reader = TileReader<T, DH, STEP>;
   constexpr int QB = STEP / 32, OB = DH / 32, NK = DH / 16, KEYS = 128;
   constexpr int kStage = 2 * Shape::kBytes + 512;          // queries, output gradients, lse2 [64], delta [64]
   extern __shared__ __align__(1024) unsigned char smem[];  // [2] stages
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
+  const Reader read(lane);
   // first keys first: under a causal mask most queries see them
   const int pairs = a.B * a.hk, pair = blockIdx.x % pairs, rest = blockIdx.x / pairs, split = rest % a.k_splits, tile = rest / a.k_splits;
   const int b = pair / a.hk, kv = pair % a.hk;
@@ -222,8 +226,8 @@ __global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
       f32x16 p = zero_block(), e = zero_block();
 #pragma unroll
       for (int kk = 0; kk < NK; ++kk) {
-        p = mma16(Shape::row_fragment(qt, 32 * qb, kk, lane), k[kk], p);
-        e = mma16(Shape::row_fragment(gt, 32 * qb, kk, lane), v[kk], e);
+        p = mma16(read.row(qt, 32 * qb, kk), k[kk], p);
+        e = mma16(read.row(gt, 32 * qb, kk), v[kk], e);
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -246,8 +250,8 @@ __global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
         const Fragment<T> pf = half_fragment<T>(p, f), ef = half_fragment<T>(e, f);
 #pragma unroll
         for (int ob = 0; ob < OB; ++ob) {
-          dv[ob] = mma16(Shape::column_fragment(gt, 32 * qb + 16 * f, 32 * ob, lane), pf, dv[ob]);
-          dk[ob] = mma16(Shape::column_fragment(qt, 32 * qb + 16 * f, 32 * ob, lane), ef, dk[ob]);
+          dv[ob] = mma16(read.column(gt, 32 * qb + 16 * f, 32 * ob), pf, dv[ob]);
+          dk[ob] = mma16(read.column(qt, 32 * qb + 16 * f, 32 * ob), ef, dk[ob]);
         }
       }
     }

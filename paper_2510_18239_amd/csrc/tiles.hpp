@@ -3,8 +3,8 @@
 //
 // A tile is ROWS rows of DH columns (the operand's own width rounded up; columns past it are zero).  Its 16-byte pieces are
 // permuted within a row by the row's number (swizzle), so that neither of the two ways it is read meets its own lanes in a bank:
-//   row_fragment     lane (n, g), slot t = tile[r0 + n][16 kk + 8g + t]            (the columns are summed)
-//   column_fragment  lane (n, g), slot t = tile[r0 + chain_k(g, t)][c0 + n]        (the rows are summed, in chained order)
+//   row      lane (n, g), slot t = tile[r0 + n][16 kk + 8g + t]       (the columns are summed)
+//   column   lane (n, g), slot t = tile[r0 + chain_k(g, t)][c0 + n]   (the rows are summed, in chained order)
 // A product's 32 x 32 accumulator, rounded to the storage type half by half (half_fragment), is the other operand of the
 // second: the two products of an attention step chain in registers.
 // fp32 tiles go through v_mfma_f32_32x32x2_f32, eight of which take the same 16-deep fragments one slot at a time.
@@ -50,40 +50,64 @@ struct Tile {
   static constexpr int kRowBytes = DH * static_cast<int>(sizeof(T)), kPieces = kRowBytes / 16, kBytes = ROWS * kRowBytes;
   static constexpr int kPerPiece = 16 / static_cast<int>(sizeof(T));
   static_assert(DH % 32 == 0 && ROWS % 16 == 0);
-  // Which piece sits in slot s of row r: s ^ swizzle(r).  Eight consecutive rows read at one column (row_fragment) and four
-  // rows at two neighbouring pieces (what sixteen lanes read in column_fragment) fall on different banks.
+  // Which piece sits in slot s of row r: s ^ swizzle(r).  Eight consecutive rows read at one column (a row fragment) and four
+  // rows at two neighbouring pieces (what sixteen lanes read for a column fragment) fall on different banks.
   __device__ static constexpr int swizzle(int r) {
     return kPieces >= 8 ? ((r & 3) << 1) | ((r >> 2) & 1) : (((r >> 1) & 1) << 1) | ((r >> 2) & 1);
   }
-  __device__ static Fragment<T> row_fragment(const unsigned char* tile, int r0, int kk, int lane) {
-    const int n = lane & 31, g = lane >> 5, s = swizzle(n);
-    const unsigned char* row = tile + (r0 + n) * kRowBytes;
+};
+
+// Where a lane's fragments begin in a tile.  The swizzle stays within 128 bytes, so that a few places and the instructions' own
+// offsets reach all of them (with a place of its own for each fragment, the widest kernels had no registers left).
+template <typename T, int DH, int ROWS>
+class TileReader {
+  using Shape = Tile<T, DH, ROWS>;
+  static constexpr int kSpan = Shape::kRowBytes < 128 ? Shape::kRowBytes : 128;  // bytes of a row that the swizzle permutes
+  static constexpr int kStep = 16 * static_cast<int>(sizeof(T));                 // bytes of 16 columns
+  static constexpr int kKs = kSpan / kStep;                                      // 16-column steps within a span
+  unsigned row_[kKs];
+  unsigned column_[sizeof(T) == 2 ? 2 : 4];
+
+ public:
+  __device__ explicit TileReader(int lane) {
+    const int n = lane & 31, g = lane >> 5;
+#pragma unroll
+    for (int kk = 0; kk < kKs; ++kk) row_[kk] = n * Shape::kRowBytes + ((kStep / 16 * kk + kStep / 32 * g) ^ Shape::swizzle(n)) * 16;
     if constexpr (sizeof(T) == 2) {
-      return *reinterpret_cast<const bf16x8*>(row + ((2 * kk + g) ^ s) * 16);
+      // ds_read_b64_tr_b16: each lane of a group of 16 gets a column of the 4 x 16 block whose rows the group's lanes point
+      // at, four lanes a row
+      const int r = 4 * g + (lane & 15) / 4, piece = 2 * ((lane >> 4) & 1) + (lane & 3) / 2;
+#pragma unroll
+      for (int odd = 0; odd < 2; ++odd)
+        column_[odd] = r * Shape::kRowBytes + ((piece + (kSpan == 128 ? 4 * odd : 0)) ^ Shape::swizzle(r)) * 16 + (lane & 1) * 8;
     } else {
-      const f32x4 lo = *reinterpret_cast<const f32x4*>(row + ((4 * kk + 2 * g) ^ s) * 16);
-      const f32x4 hi = *reinterpret_cast<const f32x4*>(row + ((4 * kk + 2 * g + 1) ^ s) * 16);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) column_[t] = (4 * g + t) * Shape::kRowBytes + ((n / 4) ^ Shape::swizzle(4 * g + t)) * 16 + (n & 3) * 4;
+    }
+  }
+  // r0 a multiple of 32
+  __device__ Fragment<T> row(const unsigned char* tile, int r0, int kk) const {
+    const unsigned char* at = tile + row_[kk % kKs] + (r0 * Shape::kRowBytes + kk / kKs * 128);
+    if constexpr (sizeof(T) == 2) {
+      return *reinterpret_cast<const bf16x8*>(at);
+    } else {
+      const f32x4 lo = *reinterpret_cast<const f32x4*>(at);
+      const f32x4 hi = *reinterpret_cast<const f32x4*>(tile + (row_[kk % kKs] ^ 16u) + (r0 * Shape::kRowBytes + kk / kKs * 128));
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     }
   }
   // r0 a multiple of 16, c0 of 32
-  __device__ static Fragment<T> column_fragment(const unsigned char* tile, int r0, int c0, int lane) {
+  __device__ Fragment<T> column(const unsigned char* tile, int r0, int c0) const {
     if constexpr (sizeof(T) == 2) {
-      // ds_read_b64_tr_b16: each lane of a group of 16 gets a column of the 4 x 16 block whose rows the group's lanes point
-      // at, four lanes a row
-      const int r = 4 * (lane >> 5) + (lane & 15) / 4, piece = c0 / 8 + 2 * ((lane >> 4) & 1) + (lane & 3) / 2;
-      const unsigned char* p = tile + (r0 + r) * kRowBytes + (piece ^ swizzle(r)) * 16 + (lane & 1) * 8;
+      const int ob = c0 / 32;
+      const unsigned char* at = tile + column_[ob % 2] + (r0 * Shape::kRowBytes + ob / 2 * 128);
       // (eight rows on, the swizzle is the same)
-      const bf16x4 lo = transposed(p), hi = transposed(p + 8 * kRowBytes);
+      const bf16x4 lo = transposed(at), hi = transposed(at + 8 * Shape::kRowBytes);
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
-      const int n = lane & 31, g = lane >> 5, piece = (c0 + n) / 4, in = n & 3;
       f32x8 v;
 #pragma unroll
-      for (int t = 0; t < 8; ++t) {
-        const int r = chain_k(g, t);
-        v[t] = *reinterpret_cast<const float*>(tile + (r0 + r) * kRowBytes + (piece ^ swizzle(r)) * 16 + in * 4);
-      }
+      for (int t = 0; t < 8; ++t) v[t] = *reinterpret_cast<const float*>(tile + column_[t & 3] + ((r0 + t / 4 * 8) * Shape::kRowBytes + c0 * 4));
       return v;
     }
   }
