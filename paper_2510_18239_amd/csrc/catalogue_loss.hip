@@ -28,7 +28,7 @@ struct Args {
   // workspace
   int32_t* live;      // [1 + rows]: how many rows have a target, and which they are
   void* packed;       // [rows][d] the rows with a target, written where some have none
-  float *c_lse2, *c_g;  // [rows] of the listed rows: lse log2 e; dloss scale
+  float *c_lse2, *c_g, *c_e;  // [rows] of the listed rows: lse log2 e; dloss scale; e of the target
   int32_t* c_target;  // [rows]
   float* parts;       // forward [splits][rows][2], dX [splits][rows][padded d], dW [splits][items][padded d]
   int splits, chunk;
@@ -72,13 +72,23 @@ __global__ __launch_bounds__(256) void gather_kernel(Args a, int64_t each) {
         if constexpr (!BACKWARD) a.loss[i] = 0.f, a.lse[i] = 0.f;
       }
     }
-    if (whole) continue;
+    if (whole && !BACKWARD) continue;
     __syncthreads();
     const int here = static_cast<int>(min<int64_t>(kGatherRows, end - at));
 #pragma unroll 4
     for (int r = wave; r < here; r += 4) {  // a wave a row
       const T* from = static_cast<const T*>(a.x) + (at + r) * a.d;
       const int to = place[r];
+      if constexpr (BACKWARD) {
+        if (to >= 0) {  // e of the row's own target, dloss scale (p - 1)
+          const T* w = static_cast<const T*>(a.w) + static_cast<int64_t>(a.targets[at + r]) * a.d;
+          float z = 0.f;
+          for (int c = lane; c < a.d; c += 64) z = fmaf(to_float(from[c]), to_float(w[c]), z);
+          z = wave_sum(z) * a.scale - a.lse[at + r];
+          if (lane == 0) a.c_e[to] = (__builtin_amdgcn_exp2f(z * kLog2e) - 1.f) * a.dloss[at + r] * a.scale;
+        }
+        if (whole) continue;
+      }
       T* dst = to >= 0 ? static_cast<T*>(a.packed) + static_cast<int64_t>(to) * a.d : static_cast<T*>(a.dx) + (at + r) * a.d;
       if (to < 0 && (!BACKWARD || a.dx == nullptr)) continue;
       if (a.x_pieces && a.quads) {  // rows of whole 16-byte pieces: at most 64 of them
@@ -147,6 +157,7 @@ __global__ __launch_bounds__(256) void catalogue_lse_kernel(Args a) {
       for (int kk = 0; kk < NK; ++kk) s[vb] = mma16(read.row(wt, 32 * vb, kk), x[kk], s[vb]);
     }
     if (v0 + (i + 1) * STEP > v1) {
+      seldom();
 #pragma unroll
       for (int vb = 0; vb < VB; ++vb)
 #pragma unroll
@@ -160,6 +171,7 @@ __global__ __launch_bounds__(256) void catalogue_lse_kernel(Args a) {
       for (int e = 0; e < 16; ++e) top = fmaxf(top, s[vb][e]);
     top = pair_max(top) * c;
     if (__any(top > m + kHeadroom)) {
+      seldom();
       const float to = fmaxf(m, top);
       l *= to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
       m = to;
@@ -241,7 +253,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void catalogue_dx_kern
       for (int kk = 0; kk < NK; ++kk) p = mma16(read.row(wt, 32 * vb, kk), x[kk], p);
 #pragma unroll
       for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(p[e], c, -lse2));
-      if (v0 + (i + 1) * STEP > v1) {  // (zero rows past the chunk: p may be infinite there)
+      if (v0 + (i + 1) * STEP > v1) {
+        seldom();  // (zero rows past the chunk: p may be infinite there)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
           if (v0 + i * STEP + 32 * vb + block_row(e, g) >= v1) p[e] = 0.f;
@@ -282,7 +295,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void catalogue_dw_kern
   using Shape = Tile<T, D, STEP>;
   using Loader = TileLoader<T, D, STEP, 4>;
   using Reader = TileReader<T, D, STEP>;
-  constexpr int RB = STEP / 32, NK = D / 16, OB = D / 32, kStage = Shape::kBytes + 1024;  // rows; lse2, dloss scale, target, each [64]
+  constexpr int RB = STEP / 32, NK = D / 16, OB = D / 32, kStage = Shape::kBytes + 1024;  // rows; lse2, dloss scale, target, its e, each [64]
   extern __shared__ __align__(1024) unsigned char smem[];                                 // [2] stages
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);
@@ -297,8 +310,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void catalogue_dw_kern
     unsigned char* at = smem + i % 2 * kStage;
     xl.issue(xm, i * STEP, i1 - i0, at, tid);
     const int from = i0 + i * STEP;
-    const void* words = wave == 0 ? static_cast<const void*>(a.c_lse2 + from) : wave == 1 ? static_cast<const void*>(a.c_g + from) : static_cast<const void*>(a.c_target + from);
-    if (wave < 3) words_to_lds(words, min(STEP, i1 - from), at + Shape::kBytes + 256 * wave, lane);
+    const void* words[4] = {a.c_lse2, a.c_g, a.c_target, a.c_e};
+    words_to_lds(static_cast<const float*>(words[wave]) + from, min(STEP, i1 - from), at + Shape::kBytes + 256 * wave, lane);
   };
   if (steps > 0) ask(0);
   Fragment<T> w[NK];
@@ -314,44 +327,55 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void catalogue_dw_kern
     const unsigned char* xt = smem + i % 2 * kStage;
     const float *lse2 = reinterpret_cast<const float*>(xt + Shape::kBytes), *weight = lse2 + 64;
     const int32_t* target = reinterpret_cast<const int32_t*>(weight + 64);
-    // whether any of the step's rows has one of the wave's items for its target (rows past the last have the weight 0)
-    const bool chosen = __any(static_cast<unsigned>(target[lane % STEP] - item0) < 32u);
+    const float* own = weight + 128;
+    // which of the step's rows have one of the wave's items for their target (rows past the last: with the weight 0)
+    const unsigned long long chosen = __ballot(lane < STEP && static_cast<unsigned>(target[lane % STEP] - item0) < 32u);
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       f32x16 e = zero_block();
 #pragma unroll
       for (int kk = 0; kk < NK; ++kk) e = mma16(read.row(xt, 32 * rb, kk), w[kk], e);
+      auto weigh = [&](auto with_targets) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int at = 32 * rb + 8 * j + 4 * g;
-        const f32x4 l4 = *reinterpret_cast<const f32x4*>(lse2 + at);
+        for (int j = 0; j < 4; ++j) {
+          const int at = 32 * rb + 8 * j + 4 * g;
+          const f32x4 l4 = *reinterpret_cast<const f32x4*>(lse2 + at), g4 = *reinterpret_cast<const f32x4*>(weight + at);
 #pragma unroll
-        for (int y = 0; y < 4; ++y) e[4 * j + y] = __builtin_amdgcn_exp2f(fmaf(e[4 * j + y], c, -l4[y]));
-        if (chosen) {
+          for (int y = 0; y < 4; ++y) e[4 * j + y] = __builtin_amdgcn_exp2f(fmaf(e[4 * j + y], c, -l4[y])) * g4[y];
+          if constexpr (with_targets) {
+            const i32x4 t4 = *reinterpret_cast<const i32x4*>(target + at);
+            const f32x4 o4 = *reinterpret_cast<const f32x4*>(own + at);
 #pragma unroll
-          for (int y = 0; y < 4; ++y)
-            if (target[at + y] == item) e[4 * j + y] -= 1.f;
+            for (int y = 0; y < 4; ++y) e[4 * j + y] = t4[y] == item ? o4[y] : e[4 * j + y];
+          }
         }
-        const f32x4 g4 = *reinterpret_cast<const f32x4*>(weight + at);
-#pragma unroll
-        for (int y = 0; y < 4; ++y) e[4 * j + y] *= g4[y];
-      }
+      };
+      if (chosen == 0) weigh(std::false_type{});
+      else weigh(std::true_type{});
 #pragma unroll
       for (int f = 0; f < 2; ++f) {
         const Fragment<T> ef = half_fragment<T>(e, f);
 #pragma unroll
         for (int ob = 0; ob < OB; ++ob) dw[ob] = mma16(read.column(xt, 32 * rb + 16 * f, 32 * ob), ef, dw[ob]);
-        // A target's e is near its row's whole weight and rarely has company: what rounding took of it is added by itself.
-        if (sizeof(T) == 2 && chosen) {
-          Fragment<T> rest;
+      }
+    }
+    // A target's e is near its row's whole weight and, in a large catalogue, rarely has company in its sum: what rounding took of it is
+    // added by itself.  (Popular items are chosen at nearly every step: sixteen rows without one of them are passed over.)
+    if (sizeof(T) == 2 && chosen != 0) {
+#pragma unroll 1
+      for (int k = 0; k < 2 * RB; ++k) {
+        if ((chosen >> (16 * k) & 0xffff) == 0) continue;
+        Fragment<T> low;
 #pragma unroll
-          for (int t = 0; t < 8; ++t) {
-            const float x = e[8 * f + t];
-            rest[t] = static_cast<std::conditional_t<sizeof(T) == 2, __bf16, float>>(target[32 * rb + block_row(8 * f + t, g)] == item ? x - static_cast<float>(ef[t]) : 0.f);
-          }
+        for (int j = 0; j < 2; ++j) {
+          const i32x4 t4 = *reinterpret_cast<const i32x4*>(target + 16 * k + 8 * j + 4 * g);
+          const f32x4 o4 = *reinterpret_cast<const f32x4*>(own + 16 * k + 8 * j + 4 * g);
 #pragma unroll
-          for (int ob = 0; ob < OB; ++ob) dw[ob] = mma16(read.column(xt, 32 * rb + 16 * f, 32 * ob), rest, dw[ob]);
+          for (int y = 0; y < 4; ++y)
+            low[4 * j + y] = static_cast<std::conditional_t<sizeof(T) == 2, __bf16, float>>(t4[y] == item ? o4[y] - static_cast<float>(static_cast<__bf16>(o4[y])) : 0.f);
         }
+#pragma unroll
+        for (int ob = 0; ob < OB; ++ob) dw[ob] = mma16(read.column(xt + 16 * k * Shape::kRowBytes, 0, 32 * ob), low, dw[ob]);
       }
     }
   }
@@ -406,7 +430,7 @@ Plan plan_of(int64_t rows, int items, int d, int dtype, bool backward) {
   const size_t by_rows = static_cast<size_t>(p.rows.splits) * rows * (backward ? D : 2) * sizeof(float);
   const size_t by_items = backward && p.items.splits > 1 ? static_cast<size_t>(p.items.splits) * items * D * sizeof(float) : 0;
   p.parts = align_up(std::max(by_rows, by_items));
-  p.bytes = p.live + p.packed + 3 * p.listed + p.parts;
+  p.bytes = p.live + p.packed + 4 * p.listed + p.parts;
   return p;
 }
 
@@ -424,6 +448,7 @@ Args args_of(const CatalogueLoss& x, const Plan& p, void* workspace) {
   a.packed = at, at += p.packed;
   a.c_lse2 = reinterpret_cast<float*>(at), at += p.listed;
   a.c_g = reinterpret_cast<float*>(at), at += p.listed;
+  a.c_e = reinterpret_cast<float*>(at), at += p.listed;
   a.c_target = reinterpret_cast<int32_t*>(at), at += p.listed;
   a.parts = reinterpret_cast<float*>(at);
   return a;
@@ -431,7 +456,7 @@ Args args_of(const CatalogueLoss& x, const Plan& p, void* workspace) {
 
 template <typename T, bool BACKWARD>
 hipError_t gather(const Args& a, hipStream_t s) {
-  const int64_t each = std::max<int64_t>(kGatherRows, (a.rows + 255) / 256);
+  const int64_t each = std::max<int64_t>(16, (a.rows + 1023) / 1024);
   hipLaunchKernelGGL((gather_kernel<T, BACKWARD>), dim3(static_cast<unsigned>((a.rows + each - 1) / each)), dim3(256), 0, s, a, each);
   return hipGetLastError();
 }

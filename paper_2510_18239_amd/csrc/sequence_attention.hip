@@ -102,6 +102,7 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_kernel(Args a) 
       for (int kk = 0; kk < NK; ++kk) s[kb] = mma16(read.row(kt, 32 * kb, kk), q[kk], s[kb]);
     }
     if (key0 + KEYS > wave_least) {
+      seldom();
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -115,6 +116,7 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_kernel(Args a) 
       for (int x = 0; x < 16; ++x) top = fmaxf(top, s[kb][x]);
     top = pair_max(top) * a.c;
     if (__any(top > m + kHeadroom)) {
+      seldom();
       const float to = fmaxf(m, top), f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
       m = to, l *= f;
 #pragma unroll

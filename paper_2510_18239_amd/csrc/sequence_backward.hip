@@ -128,6 +128,7 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
 #pragma unroll
       for (int x = 0; x < 16; ++x) e[x] = __builtin_amdgcn_exp2f(fmaf(s[x], c, -lse2)) * (e[x] - delta);
       if (partial) {
+        seldom();
 #pragma unroll
         for (int x = 0; x < 16; ++x)
           if (key0 + 32 * kb + block_row(x, g) >= limit) e[x] = 0.f;
@@ -239,6 +240,7 @@ __global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
         }
       }
       if (partial) {
+        seldom();
 #pragma unroll
         for (int x = 0; x < 16; ++x) {
           const int query = q0 + 32 * qb + block_row(x, g);

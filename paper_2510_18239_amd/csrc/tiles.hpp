@@ -18,6 +18,7 @@ namespace lime {
 
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 template <typename T>
 using Fragment = std::conditional_t<std::is_same_v<T, float>, f32x8, bf16x8>;
@@ -42,6 +43,9 @@ __device__ __forceinline__ Fragment<T> half_fragment(const f32x16& d, int f) {
   for (int t = 0; t < 8; ++t) r[t] = static_cast<std::conditional_t<std::is_same_v<T, float>, float, __bf16>>(d[8 * f + t]);
   return r;
 }
+// Stands first in a branch that few tiles take (masks): keeps the compiler from computing it for all of them and selecting after,
+// which cost as many vector instructions again as the softmax itself.
+__device__ __forceinline__ void seldom() { asm volatile(""); }
 // Row of a 32 x 32 accumulator that register i of lane half g holds.
 __device__ __forceinline__ constexpr int block_row(int i, int g) { return 8 * (i >> 2) + 4 * g + (i & 3); }
 
@@ -133,12 +137,14 @@ struct TileLoader {
   using Shape = Tile<T, DH, ROWS>;
   static constexpr int kLoads = Shape::kBytes / 1024 / WAVES;  // a wave's, for one tile
   static_assert(kLoads * WAVES * 1024 == Shape::kBytes && ROWS <= 128);
-  unsigned offset[kLoads];
+  static constexpr int kRowsALoad = WAVES * 1024 / Shape::kRowBytes;               // from one of a wave's loads to its next
+  static constexpr int kOffsets = kRowsALoad >= 8 ? 1 : 8 / kRowsALoad < kLoads ? 8 / kRowsALoad : kLoads;  // the swizzle repeats after eight rows
+  unsigned offset[kOffsets];
 
   __device__ void init(const Rows& m, int tid) {
     const int lane = tid & 63, wave = tid >> 6;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
+    for (int i = 0; i < kOffsets; ++i) {
       const int at = (wave + WAVES * i) * 64 + lane, row = at / Shape::kPieces, piece = (at % Shape::kPieces) ^ Shape::swizzle(row);
       offset[i] = piece * 16u < m.width ? row * m.stride + piece * 16u : 0x80000000u;
     }
@@ -159,8 +165,13 @@ struct TileLoader {
       const unsigned lds = __builtin_amdgcn_readfirstlane(lds_offset_of(tile) + (tid >> 6) * 1024);
 #pragma unroll
       for (int i = 0; i < kLoads; ++i)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                     : : "s"(lds + WAVES * 1024 * i), "v"(offset[i]), "s"(resource) : "memory");
+{
+        unsigned at_row;  // (added here, not by the compiler: it would keep all the sums in registers across the kernel's loop)
+        asm volatile("s_mov_b32 m0, %1\n\tv_add_u32_e32 %0, %2, %3\n\tbuffer_load_dwordx4 %0, %4, 0 offen lds"
+                     : "=&v"(at_row)
+                     : "s"(lds + WAVES * 1024 * i), "s"(i / kOffsets * kOffsets * kRowsALoad * m.stride), "v"(offset[i % kOffsets]), "s"(resource)
+                     : "memory");
+      }
     } else {
       const unsigned columns = m.width / sizeof(T);
       for (unsigned i = tid; i < ROWS * DH; i += WAVES * 64) {
