@@ -141,7 +141,7 @@ __global__ __launch_bounds__(256) void catalogue_lse_kernel(Args a) {
   const float c = fmaxf(fabsf(a.scale) * kLog2e, 1e-37f);
   if (a.scale < 0.f) {
 #pragma unroll
-    for (int kk = 0; kk < NK; ++kk) x[kk] = -x[kk];
+    for (int kk = 0; kk < NK; ++kk) negate(x[kk]);
   }
   float m = -INFINITY, l = 0.f;
   for (int i = 0; i < steps; ++i) {
@@ -361,18 +361,19 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void catalogue_dw_kern
     }
     // A target's e is near its row's whole weight and, in a large catalogue, rarely has company in its sum: what rounding took of it is
     // added by itself.  (Popular items are chosen at nearly every step: sixteen rows without one of them are passed over.)
-    if (sizeof(T) == 2 && chosen != 0) {
+    if constexpr (sizeof(T) == 2) {
+      if (chosen != 0)
 #pragma unroll 1
       for (int k = 0; k < 2 * RB; ++k) {
         if ((chosen >> (16 * k) & 0xffff) == 0) continue;
-        Fragment<T> low;
+        bf16x8 low;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const i32x4 t4 = *reinterpret_cast<const i32x4*>(target + 16 * k + 8 * j + 4 * g);
           const f32x4 o4 = *reinterpret_cast<const f32x4*>(own + 16 * k + 8 * j + 4 * g);
 #pragma unroll
           for (int y = 0; y < 4; ++y)
-            low[4 * j + y] = static_cast<std::conditional_t<sizeof(T) == 2, __bf16, float>>(t4[y] == item ? o4[y] - static_cast<float>(static_cast<__bf16>(o4[y])) : 0.f);
+            low[4 * j + y] = static_cast<__bf16>(t4[y] == item ? o4[y] - static_cast<float>(static_cast<__bf16>(o4[y])) : 0.f);
         }
 #pragma unroll
         for (int ob = 0; ob < OB; ++ob) dw[ob] = mma16(read.column(xt + 16 * k * Shape::kRowBytes, 0, 32 * ob), low, dw[ob]);

@@ -79,7 +79,7 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_kernel(Args a) 
   load_row<T, DH>(qp, width, a.pieces, live, g, q);
   if (a.negate) {
 #pragma unroll
-    for (int kk = 0; kk < NK; ++kk) q[kk] = -q[kk];
+    for (int kk = 0; kk < NK; ++kk) negate(q[kk]);
   }
   f32x16 o[OB];
 #pragma unroll

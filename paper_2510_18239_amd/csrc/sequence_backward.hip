@@ -98,7 +98,7 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk)
 #pragma unroll
-      for (int t = 0; t < 8; ++t) delta = fmaf(static_cast<float>(go[kk][t]), static_cast<float>(o[kk][t]), delta);
+      for (int t = 0; t < 8; ++t) delta = fmaf(element(go[kk], t), element(o[kk], t), delta);
     delta = pair_sum(delta);
   }
   if (live && g == 0 && split == 0) {

@@ -7,7 +7,10 @@
 //   column   lane (n, g), slot t = tile[r0 + chain_k(g, t)][c0 + n]   (the rows are summed, in chained order)
 // A product's 32 x 32 accumulator, rounded to the storage type half by half (half_fragment), is the other operand of the
 // second: the two products of an attention step chain in registers.
-// fp32 tiles go through v_mfma_f32_32x32x2_f32, eight of which take the same 16-deep fragments one slot at a time.
+// fp32 operands are cut into three bf16 parts of eight bits each, which is all of their 24 bits, and a product is the six products of
+// parts that reach into them (the three left out are below 2^-24 of it): six bf16 instructions of 32 cycles where
+// v_mfma_f32_32x32x2_f32 takes eight of 64, and the cutting is done beside them by the vector units.  An operand that is not finite
+// gives NaN; one below 2^-110 loses its last parts to the instruction's range.
 #pragma once
 
 #include <type_traits>
@@ -20,14 +23,46 @@ typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
+struct Parts {  // an fp32 fragment: x = sum of its parts
+  bf16x8 part[3];
+};
 template <typename T>
-using Fragment = std::conditional_t<std::is_same_v<T, float>, f32x8, bf16x8>;
+using Fragment = std::conditional_t<std::is_same_v<T, float>, Parts, bf16x8>;
+
+__device__ __forceinline__ Parts in_parts(const f32x8& x) {
+  u32x4 w[3];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    unsigned bits[3][2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {  // the leading eight bits, the next eight, the rest: no rounding
+      const float v = x[2 * i + k];
+      bits[0][k] = __float_as_uint(v) & 0xffff0000u;
+      const float r = v - __uint_as_float(bits[0][k]);
+      bits[1][k] = __float_as_uint(r) & 0xffff0000u;
+      bits[2][k] = __float_as_uint(r - __uint_as_float(bits[1][k]));
+    }
+#pragma unroll
+    for (int p = 0; p < 3; ++p) w[p][i] = __builtin_amdgcn_perm(bits[p][1], bits[p][0], 0x07060302);  // the upper halves
+  }
+  return {__builtin_bit_cast(bf16x8, w[0]), __builtin_bit_cast(bf16x8, w[1]), __builtin_bit_cast(bf16x8, w[2])};
+}
 
 __device__ __forceinline__ f32x16 mma16(bf16x8 a, bf16x8 b, f32x16 c) { return mfma32(a, b, c); }
-__device__ __forceinline__ f32x16 mma16(f32x8 a, f32x8 b, f32x16 c) {
+__device__ __forceinline__ f32x16 mma16(const Parts& a, const Parts& b, f32x16 c) {
+  c = mfma32(a.part[0], b.part[2], c);  // the small ones first
+  c = mfma32(a.part[1], b.part[1], c);
+  c = mfma32(a.part[2], b.part[0], c);
+  c = mfma32(a.part[0], b.part[1], c);
+  c = mfma32(a.part[1], b.part[0], c);
+  return mfma32(a.part[0], b.part[0], c);
+}
+__device__ __forceinline__ float element(const bf16x8& f, int t) { return static_cast<float>(f[t]); }
+__device__ __forceinline__ float element(const Parts& f, int t) { return static_cast<float>(f.part[0][t]) + (static_cast<float>(f.part[1][t]) + static_cast<float>(f.part[2][t])); }
+__device__ __forceinline__ void negate(bf16x8& f) { f = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, f) ^ 0x80008000u); }
+__device__ __forceinline__ void negate(Parts& f) {
 #pragma unroll
-  for (int t = 0; t < 8; ++t) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[t], b[t], c, 0, 0, 0);
-  return c;
+  for (int p = 0; p < 3; ++p) negate(f.part[p]);
 }
 __device__ __forceinline__ f32x16 zero_block() {
   f32x16 z;
@@ -38,10 +73,14 @@ __device__ __forceinline__ f32x16 zero_block() {
 // Registers 8f .. 8f + 7 of an accumulator as a fragment of the storage type (bf16: round to nearest even).
 template <typename T>
 __device__ __forceinline__ Fragment<T> half_fragment(const f32x16& d, int f) {
-  Fragment<T> r;
+  if constexpr (sizeof(T) == 2) {
+    return pack_half(d, f);
+  } else {
+    f32x8 r;
 #pragma unroll
-  for (int t = 0; t < 8; ++t) r[t] = static_cast<std::conditional_t<std::is_same_v<T, float>, float, __bf16>>(d[8 * f + t]);
-  return r;
+    for (int t = 0; t < 8; ++t) r[t] = d[8 * f + t];
+    return in_parts(r);
+  }
 }
 // Stands first in a branch that few tiles take (masks): keeps the compiler from computing it for all of them and selecting after,
 // which cost as many vector instructions again as the softmax itself.
@@ -97,7 +136,7 @@ class TileReader {
     } else {
       const f32x4 lo = *reinterpret_cast<const f32x4*>(at);
       const f32x4 hi = *reinterpret_cast<const f32x4*>(tile + (row_[kk % kKs] ^ 16u) + (r0 * Shape::kRowBytes + kk / kKs * 128));
-      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      return in_parts(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
   }
   // r0 a multiple of 16, c0 of 32
@@ -112,7 +151,7 @@ class TileReader {
       f32x8 v;
 #pragma unroll
       for (int t = 0; t < 8; ++t) v[t] = *reinterpret_cast<const float*>(tile + column_[t & 3] + ((r0 + t / 4 * 8) * Shape::kRowBytes + c0 * 4));
-      return v;
+      return in_parts(v);
     }
   }
 
@@ -203,28 +242,31 @@ __device__ __forceinline__ void load_row(const void* row, unsigned width, bool p
 #pragma unroll
   for (int kk = 0; kk < DH / 16; ++kk) {
     const int c = 16 * kk + 8 * g;
-    Fragment<T> v;
-#pragma unroll
-    for (int t = 0; t < 8; ++t) v[t] = 0;
     const T* p = static_cast<const T*>(row) + c;
-    if (pieces) {
-      if constexpr (sizeof(T) == 2) {
-        if (live && c * 2u < width) v = *reinterpret_cast<const bf16x8*>(p);
-      } else {
+    if constexpr (sizeof(T) == 2) {
+      u32x4 v = {0, 0, 0, 0};
+      if (pieces) {
+        if (live && c * 2u < width) v = *reinterpret_cast<const u32x4*>(p);
+      } else if (live) {
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+          if ((c + t) * 2u < width) v[t / 2] |= static_cast<unsigned>(p[t].bits) << (16 * (t & 1));
+      }
+      f[kk] = __builtin_bit_cast(bf16x8, v);
+    } else {
+      f32x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
+      if (pieces) {
         f32x4 lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
         if (live && c * 4u < width) lo = *reinterpret_cast<const f32x4*>(p);
         if (live && (c + 4) * 4u < width) hi = *reinterpret_cast<const f32x4*>(p + 4);
         v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      }
-    } else if (live) {
+      } else if (live) {
 #pragma unroll
-      for (int t = 0; t < 8; ++t)
-        if ((c + t) * sizeof(T) < width) {
-          if constexpr (sizeof(T) == 2) v[t] = __builtin_bit_cast(__bf16, p[t].bits);
-          else v[t] = p[t];
-        }
+        for (int t = 0; t < 8; ++t)
+          if ((c + t) * 4u < width) v[t] = p[t];
+      }
+      f[kk] = in_parts(v);
     }
-    f[kk] = v;
   }
 }
 
