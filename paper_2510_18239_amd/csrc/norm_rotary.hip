@@ -16,7 +16,7 @@
 namespace lime {
 namespace {
 
-constexpr int kRows = 8, kBackRows = 32;  // rows of a workgroup's turn, forward and backward
+constexpr int kRows = 8, kBackRows = 32;  // the most rows of a workgroup's turn, forward and backward
 constexpr int kMaxGroups = 1024; // workgroups of a backward pass: each leaves one partial sum of the weights' gradients
 constexpr int kMaxHalf = kMaxRotaryHead / 2;
 
@@ -30,6 +30,7 @@ struct Args {
   const int32_t* positions;
   int64_t rows;
   int dh, lanes;    // lanes of a head, a power of two
+  int turn;         // rows of a workgroup's turn
   float eps;
   float* partial;   // [2][dh][groups]
   double turns[kMaxHalf];  // base^(-2 i / dh) / (2 pi)
@@ -70,13 +71,13 @@ __device__ __forceinline__ float lanes_sum(float x, int lanes) {
 
 // A lane's part of a head: PARTS pieces of VEC elements of the first half, and their partners.
 template <typename T, int VEC, int PARTS, bool BACKWARD, int ROWS>
-__global__ __launch_bounds__(256) void norm_rotary_kernel(Args a) {
+__global__ __launch_bounds__(256, BACKWARD ? 4 : 1) void norm_rotary_kernel(Args a) {
   __shared__ float2 turned[ROWS][kMaxHalf];  // cosine, sine
   __shared__ float sums[BACKWARD ? 4 : 1][2][kMaxRotaryHead];  // of the waves
   const int tid = threadIdx.x, half = a.dh / 2, t = tid % a.lanes, unit = tid / a.lanes, units = 256 / a.lanes;
   float dgamma[BACKWARD ? 2 : 1][2][PARTS][VEC] = {};  // side, half
-  for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * ROWS; row0 < a.rows; row0 += static_cast<int64_t>(gridDim.x) * ROWS) {
-    const int count = static_cast<int>(min<int64_t>(ROWS, a.rows - row0));
+  for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * a.turn; row0 < a.rows; row0 += static_cast<int64_t>(gridDim.x) * a.turn) {
+    const int count = static_cast<int>(min<int64_t>(a.turn, a.rows - row0));
     __syncthreads();  // everyone is done with the last rows' angles
     for (int i = tid; i < count * half; i += 256) {
       const int r = i / half, c = i % half;
@@ -91,44 +92,51 @@ __global__ __launch_bounds__(256) void norm_rotary_kernel(Args a) {
 #pragma unroll
     for (int side = 0; side < 2; ++side) {
       const int heads = a.heads[side];
+      float glo[PARTS][VEC], ghi[PARTS][VEC];
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) {
+        const int c = (t + p * a.lanes) * VEC;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) glo[p][i] = ghi[p][i] = 1.f;
+        if (a.gamma[side] && c < half) {
+          load_piece<T, VEC>(static_cast<const T*>(a.gamma[side]) + c, glo[p]);
+          load_piece<T, VEC>(static_cast<const T*>(a.gamma[side]) + half + c, ghi[p]);
+        }
+      }
       for (int u = unit; u < count * heads; u += units) {
         const int r = u / heads, head = u % heads;
         const T* x = static_cast<const T*>(a.x[side]) + (row0 + r) * a.x_stride[side] + head * a.dh;
-        float lo[PARTS][VEC], hi[PARTS][VEC], square = 0.f;
-#pragma unroll
-        for (int p = 0; p < PARTS; ++p) {
-          const int c = (t + p * a.lanes) * VEC;
-          if (c < half) {
-            load_piece<T, VEC>(x + c, lo[p]), load_piece<T, VEC>(x + half + c, hi[p]);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) square = fmaf(lo[p][i], lo[p][i], fmaf(hi[p][i], hi[p][i], square));
-          }
-        }
-        const float inverse = 1.f / sqrtf(lanes_sum(square, a.lanes) / a.dh + a.eps);
-        float glo[PARTS][VEC], ghi[PARTS][VEC], mean = 0.f;
+        const T* dy = BACKWARD ? static_cast<const T*>(a.dy[side]) + (row0 + r) * a.dy_stride[side] + head * a.dh : nullptr;
+        float lo[PARTS][VEC], hi[PARTS][VEC], ylo[BACKWARD ? PARTS : 1][VEC], yhi[BACKWARD ? PARTS : 1][VEC], square = 0.f;
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
           const int c = (t + p * a.lanes) * VEC;
           if (c >= half) continue;
+          load_piece<T, VEC>(x + c, lo[p]), load_piece<T, VEC>(x + half + c, hi[p]);
+          if constexpr (BACKWARD) load_piece<T, VEC>(dy + c, ylo[p]), load_piece<T, VEC>(dy + half + c, yhi[p]);
+        }
 #pragma unroll
-          for (int i = 0; i < VEC; ++i) glo[p][i] = ghi[p][i] = 1.f;
-          if (a.gamma[side]) {
-            load_piece<T, VEC>(static_cast<const T*>(a.gamma[side]) + c, glo[p]);
-            load_piece<T, VEC>(static_cast<const T*>(a.gamma[side]) + half + c, ghi[p]);
-          }
+        for (int p = 0; p < PARTS; ++p) {
+          if ((t + p * a.lanes) * VEC >= half) continue;
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) square = fmaf(lo[p][i], lo[p][i], fmaf(hi[p][i], hi[p][i], square));
+        }
+        const float inverse = 1.f / sqrtf(lanes_sum(square, a.lanes) / a.dh + a.eps);
+        float mean = 0.f;
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+          const int c = (t + p * a.lanes) * VEC;
+          if (c >= half) continue;
           if constexpr (BACKWARD) {
-            const T* dy = static_cast<const T*>(a.dy[side]) + (row0 + r) * a.dy_stride[side] + head * a.dh;
-            float ylo[VEC], yhi[VEC];
-            load_piece<T, VEC>(dy + c, ylo), load_piece<T, VEC>(dy + half + c, yhi);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
               const float2 w = turned[r][c + i];
-              const float dlo = fmaf(ylo[i], w.x, yhi[i] * w.y), dhi = fmaf(yhi[i], w.x, -ylo[i] * w.y);
+              const float dlo = fmaf(ylo[p][i], w.x, yhi[p][i] * w.y), dhi = fmaf(yhi[p][i], w.x, -ylo[p][i] * w.y);
               lo[p][i] *= inverse, hi[p][i] *= inverse;
               dgamma[side][0][p][i] = fmaf(dlo, lo[p][i], dgamma[side][0][p][i]);
               dgamma[side][1][p][i] = fmaf(dhi, hi[p][i], dgamma[side][1][p][i]);
-              glo[p][i] *= dlo, ghi[p][i] *= dhi;  // dn
-              mean = fmaf(glo[p][i], lo[p][i], fmaf(ghi[p][i], hi[p][i], mean));
+              ylo[p][i] = glo[p][i] * dlo, yhi[p][i] = ghi[p][i] * dhi;  // dn
+              mean = fmaf(ylo[p][i], lo[p][i], fmaf(yhi[p][i], hi[p][i], mean));
             }
           } else {
 #pragma unroll
@@ -147,7 +155,7 @@ __global__ __launch_bounds__(256) void norm_rotary_kernel(Args a) {
           if (c >= half) continue;
           if constexpr (BACKWARD) {
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) lo[p][i] = inverse * fmaf(-mean, lo[p][i], glo[p][i]), hi[p][i] = inverse * fmaf(-mean, hi[p][i], ghi[p][i]);
+            for (int i = 0; i < VEC; ++i) lo[p][i] = inverse * fmaf(-mean, lo[p][i], ylo[p][i]), hi[p][i] = inverse * fmaf(-mean, hi[p][i], yhi[p][i]);
           }
           store_piece<T, VEC>(out + c, lo[p]), store_piece<T, VEC>(out + half + c, hi[p]);
         }
@@ -184,13 +192,16 @@ __global__ __launch_bounds__(256) void norm_rotary_fold_kernel(const float* part
   if (side > 1) return;
   T* to = side ? dk : dq;
   float total = 0.f;
+#pragma unroll 8
   for (int i = lane; i < groups; i += 64) total += partial[static_cast<int64_t>(at) * groups + i];
   total = wave_sum(total);
   if (to && lane == 0) store_as(to + c, total);
 }
 
 bool multiple(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
-int64_t groups_of(int64_t rows) { return std::min<int64_t>(kMaxGroups, (rows + kBackRows - 1) / kBackRows); }
+// Few rows are spread over more workgroups, in shorter turns.
+int back_turn(int64_t rows) { return static_cast<int>(std::clamp<int64_t>((rows + kMaxGroups - 1) / kMaxGroups, 4, kBackRows)); }
+int64_t groups_of(int64_t rows) { return std::min<int64_t>(kMaxGroups, (rows + back_turn(rows) - 1) / back_turn(rows)); }
 
 template <typename T, int VEC, int PARTS>
 hipError_t launch(const Args& a, bool backward, hipStream_t s) {
@@ -214,7 +225,7 @@ hipError_t run(const NormRotary& x, void* workspace, bool backward, hipStream_t 
     vectors = vectors && multiple(x.x[i], 16) && multiple(x.dy[i], 16) && multiple(x.out[i], 16) && multiple(x.gamma[i], 16) &&
               x.x_stride[i] * e % 16 == 0 && x.dy_stride[i] * e % 16 == 0 && x.out_stride[i] * e % 16 == 0;
   }
-  a.positions = x.positions, a.rows = x.rows, a.dh = x.dh, a.eps = x.eps, a.partial = static_cast<float*>(workspace);
+  a.positions = x.positions, a.rows = x.rows, a.dh = x.dh, a.eps = x.eps, a.turn = backward ? back_turn(x.rows) : kRows, a.partial = static_cast<float*>(workspace);
   const long double ratio = powl(x.base, -2.0L / x.dh);
   long double f = 1.0L / (2.0L * 3.14159265358979323846264338327950288L);
   for (int i = 0; i < half; ++i, f *= ratio) a.turns[i] = static_cast<double>(f);
