@@ -15,12 +15,12 @@ namespace {
 struct Args {
   const void *q, *k, *v;
   int64_t q_stride, k_stride, v_stride;  // elements
-  const int32_t *q_offsets, *q_lens, *k_offsets, *k_lens;
+  Packing where;
   void* o;
   float* lse;
   float *part_o, *part_ml;  // splits > 1: [splits][B][hk][max_q group][padded dh], [...][2]
-  int64_t q_rows, k_rows;
-  int B, max_q, max_k, hq, hk, group, dh, tiles, splits, chunk;
+  Divisor group, splits;    // query heads of a key head; chunks of the keys
+  int B, hq, hk, dh, tiles, chunk;
   float c;                  // |scale| log2 e
   bool negate, pieces, causal, quads;
 };
@@ -39,24 +39,24 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_kernel(Args a) 
   extern __shared__ __align__(1024) unsigned char smem[];  // [STAGES][keys, values]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);
-  // users and key heads fastest: the workgroups of one of them, which read the same keys, land on the same XCD where their number
+  // key heads and users fastest: the workgroups of one of them, which read the same keys, land on the same XCD where their number
   // is a multiple of eight; last tiles of rows first, under a causal mask the longest
-  const int pairs = a.B * a.hk, pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
-  const int split = rest % a.splits, tile = a.tiles - 1 - rest / a.splits;
-  const int b = pair / a.hk, kv = pair % a.hk;
-  const Span qs = span_of(a.q_offsets, a.q_lens, b, a.q_rows, a.max_q), ks = span_of(a.k_offsets, a.k_lens, b, a.k_rows, a.max_k);
-  const int r0 = tile * ROWS, slot_rows = qs.slot * a.group, used_rows = qs.used * a.group;
+  const int kv = blockIdx.x, b = blockIdx.y, pairs = a.B * a.hk, pair = b * a.hk + kv, group = a.group.d, splits = a.splits.d;
+  const int reversed = splits > 1 ? a.splits.divide(blockIdx.z) : blockIdx.z, split = blockIdx.z - reversed * splits, tile = a.tiles - 1 - reversed;
+  const auto [qs, ks] = spans_of(a.where, b);
+  const int r0 = tile * ROWS, slot_rows = qs.slot * group, used_rows = qs.used * group;
   if (r0 >= slot_rows) return;
   // this lane's row
-  const int r = r0 + 32 * wave + n, query = r / a.group, head = kv * a.group + r % a.group;
+  const int r = r0 + 32 * wave + n, query = a.group.divide(r), head = kv * group + r - query * group;
   const bool live = r < used_rows;
-  const int limit = live ? keys_seen(query, qs.used, ks.used, a.causal) : 0;
+  const int n_q = qs.used, n_k = ks.used;
+  const int limit = live ? keys_seen(query, n_q, n_k, a.causal) : 0;
   // the furthest any row of the wave, of the workgroup, sees, and the least that a live row of the wave does
-  auto last_limit = [&](int rows_end) { return rows_end > 0 ? keys_seen((rows_end - 1) / a.group, qs.used, ks.used, a.causal) : 0; };
+  auto last_limit = [&, n_q = n_q, n_k = n_k](int rows_end) { return rows_end > 0 ? keys_seen(a.group.divide(rows_end - 1), n_q, n_k, a.causal) : 0; };
   const int w0 = r0 + 32 * wave, wave_most = w0 < used_rows ? last_limit(min(w0 + 32, used_rows)) : 0;
-  const int wave_least = w0 + 32 <= used_rows ? keys_seen(w0 / a.group, qs.used, ks.used, a.causal) : 0;
+  const int wave_least = w0 + 32 <= used_rows ? keys_seen(a.group.divide(w0), n_q, n_k, a.causal) : 0;
   const int most = r0 < used_rows ? last_limit(min(r0 + ROWS, used_rows)) : 0;
-  const int k_begin = split * a.chunk, k_end = a.splits > 1 ? min(most, k_begin + a.chunk) : most;
+  const int k_begin = split * a.chunk, k_end = splits > 1 ? min(most, k_begin + a.chunk) : most;
   const int steps = k_end > k_begin ? (k_end - k_begin + KEYS - 1) / KEYS : 0;
 
   const T* kp = static_cast<const T*>(a.k) + (ks.start + k_begin) * a.k_stride + kv * a.dh;
@@ -142,8 +142,8 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_kernel(Args a) 
   }
   l = pair_sum(l);
   if (r >= slot_rows) return;
-  if (a.splits > 1) {
-    const int64_t at = (static_cast<int64_t>(split) * pairs + pair) * (static_cast<int64_t>(a.max_q) * a.group) + r;
+  if (splits > 1) {
+    const int64_t at = (static_cast<int64_t>(split) * pairs + pair) * (static_cast<int64_t>(a.where.max_q) * group) + r;
 #pragma unroll
     for (int ob = 0; ob < OB; ++ob) store_block(a.part_o + at * DH, o[ob], 1.f, 32 * ob, DH, true, g);
     if (g == 0) a.part_ml[at * 2] = m, a.part_ml[at * 2 + 1] = l;
@@ -163,11 +163,11 @@ __global__ __launch_bounds__(256) void sequence_attention_merge_kernel(Args a, i
   __shared__ f32x4 met[256];
   __shared__ float met_m[256], met_l[256];
   const Folder<DH> at(groups);
-  const int pairs = a.B * a.hk, pair = blockIdx.x % pairs, b = pair / a.hk, kv = pair % a.hk;
-  const int r = static_cast<int>(blockIdx.x / pairs) * at.rows + at.row;
-  const Span qs = span_of(a.q_offsets, a.q_lens, b, a.q_rows, a.max_q);
-  const bool live = r < qs.slot * a.group;
-  const int64_t each = static_cast<int64_t>(a.max_q) * a.group, step = pairs * each, state = pair * each + r;
+  const int kv = blockIdx.x, b = blockIdx.y, pairs = a.B * a.hk, pair = b * a.hk + kv, group = a.group.d, splits = a.splits.d;
+  const int r = blockIdx.z * at.rows + at.row;
+  const Span qs = spans_of(a.where, b).q;
+  const bool live = r < qs.slot * group;
+  const int64_t each = static_cast<int64_t>(a.where.max_q) * group, step = pairs * each, state = pair * each + r;
   float m = -INFINITY, l = 0.f;
   f32x4 o = {0, 0, 0, 0};
   auto add = [&](float m1, float l1, const f32x4& o1) {
@@ -179,7 +179,7 @@ __global__ __launch_bounds__(256) void sequence_attention_merge_kernel(Args a, i
   };
   if (live) {
 #pragma unroll 4
-    for (int s = at.group; s < a.splits; s += groups) {
+    for (int s = at.group; s < splits; s += groups) {
       const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (state + s * step) * 2);
       add(ml.x, ml.y, *reinterpret_cast<const f32x4*>(a.part_o + (state + s * step) * DH + 4 * at.t));
     }
@@ -195,7 +195,8 @@ __global__ __launch_bounds__(256) void sequence_attention_merge_kernel(Args a, i
   }
   if (!live || at.group != 0) return;
   const float inverse = l == 0.f ? 0.f : 1.f / l;
-  const int64_t row = (qs.start + r / a.group) * a.hq + kv * a.group + r % a.group;
+  const int query = a.group.divide(r);
+  const int64_t row = (qs.start + query) * a.hq + kv * group + r - query * group;
 #pragma unroll
   for (int j = 0; j < 4; ++j) o[j] *= inverse;
   store_four(static_cast<T*>(a.o) + row * a.dh, o, 4 * at.t, a.dh, a.quads);
@@ -215,10 +216,10 @@ Plan plan_of(const SequenceAttention& a) {
   Plan p{};
   p.dh = dh <= 32 ? 32 : dh <= 64 ? 64 : 128;
   p.waves = rows <= 32 ? 1 : 4;
-  p.keys = dtype == 1 ? 64 : 32;
+  p.keys = dtype == 1 && p.waves > 1 ? 64 : 32;
   p.tiles = static_cast<int>((rows + 32 * p.waves - 1) / (32 * p.waves));
   const int64_t groups = B * hk * p.tiles;
-  const int64_t want = (p.waves == 1 ? 8 : 2) * static_cast<int64_t>(compute_units());
+  const int64_t want = (p.waves == 1 ? 4 : 2) * static_cast<int64_t>(compute_units());
   int64_t splits = groups >= want ? 1 : std::min((want + groups - 1) / groups, (max_k + 255) / 256);
   int64_t chunk = (max_k + splits - 1) / splits;
   chunk = (chunk + p.keys - 1) / p.keys * p.keys;
@@ -233,24 +234,23 @@ Plan plan_of(const SequenceAttention& a) {
 }
 
 template <typename T, int DH, int WAVES, int KEYS, int STAGES>
-hipError_t launch(const Args& a, int64_t blocks, hipStream_t s) {
+hipError_t launch(const Args& a, hipStream_t s) {
   constexpr int lds = STAGES * 2 * Tile<T, DH, KEYS>::kBytes;
   static PerDevice granted;
   const auto kernel = sequence_attention_kernel<T, DH, WAVES, KEYS, STAGES>;
   if (hipError_t e = allow_lds(granted, reinterpret_cast<const void*>(kernel), lds); e != hipSuccess) return e;
-  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks)), dim3(WAVES * 64), lds, s, a);
+  hipLaunchKernelGGL(kernel, dim3(a.hk, a.B, a.tiles * a.splits.d), dim3(WAVES * 64), lds, s, a);
   return hipGetLastError();
 }
 
 template <typename T, int DH>
 hipError_t run(const Args& a, const Plan& p, hipStream_t s) {
   constexpr int KEYS = sizeof(T) == 2 ? 64 : 32;
-  const int64_t pairs = static_cast<int64_t>(a.B) * a.hk, blocks = pairs * a.tiles * a.splits;
-  hipError_t e = p.waves == 1 ? launch<T, DH, 1, KEYS, 2>(a, blocks, s) : launch<T, DH, 4, KEYS, 2>(a, blocks, s);
-  if (e != hipSuccess || a.splits == 1) return e;
-  const int groups = fold_groups(a.splits, DH / 4);
-  const int64_t rows = static_cast<int64_t>(a.max_q) * a.group, per = 256 / (DH / 4) / groups;
-  hipLaunchKernelGGL((sequence_attention_merge_kernel<T, DH>), dim3(static_cast<unsigned>(pairs * ((rows + per - 1) / per))), dim3(256), 0, s, a, groups);
+  hipError_t e = p.waves == 1 ? launch<T, DH, 1, 32, sizeof(T) == 2 ? 4 : 2>(a, s) : launch<T, DH, 4, KEYS, 2>(a, s);
+  if (e != hipSuccess || a.splits.d == 1) return e;
+  const int groups = fold_groups(a.splits.d, DH / 4);
+  const int64_t rows = static_cast<int64_t>(a.where.max_q) * a.group.d, per = 256 / (DH / 4) / groups;
+  hipLaunchKernelGGL((sequence_attention_merge_kernel<T, DH>), dim3(a.hk, a.B, static_cast<unsigned>((rows + per - 1) / per)), dim3(256), 0, s, a, groups);
   return hipGetLastError();
 }
 
@@ -258,11 +258,12 @@ bool multiple(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) %
 
 }  // namespace
 
-bool sequence_attention_fits(const SequenceAttention& a) {  // 2^32 work items a launch
+bool sequence_attention_fits(const SequenceAttention& a) {  // 2^32 work items a launch, 65535 workgroups along the grid's third axis
   const int64_t rows = static_cast<int64_t>(a.max_q) * (a.hq / a.hk), pairs = static_cast<int64_t>(a.B) * a.hk;
   if (rows >= (int64_t{1} << 31) - 128 || pairs >= (int64_t{1} << 24)) return false;
   const Plan p = plan_of(a);
-  return pairs * p.tiles * p.splits < (int64_t{1} << 26) / p.waves && (p.splits == 1 || pairs * rows < (int64_t{1} << 24));
+  const int64_t deep = static_cast<int64_t>(p.tiles) * p.splits;
+  return deep < 65536 && pairs * deep < (int64_t{1} << 26) / p.waves && (p.splits == 1 || (rows < 65536 && pairs * rows < (int64_t{1} << 24)));
 }
 
 size_t sequence_attention_workspace(const SequenceAttention& a) { return std::max<size_t>(plan_of(a).bytes, 256); }
@@ -272,11 +273,10 @@ hipError_t sequence_attention(const SequenceAttention& x, void* workspace, hipSt
   const size_t e = x.dtype == 1 ? 2 : 4;
   Args a{};
   a.q = x.Q, a.k = x.K, a.v = x.V, a.q_stride = x.q_stride, a.k_stride = x.k_stride, a.v_stride = x.v_stride;
-  a.q_offsets = x.q_offsets, a.q_lens = x.q_lens, a.k_offsets = x.k_offsets, a.k_lens = x.k_lens;
-  a.o = x.O, a.lse = x.lse, a.q_rows = x.q_rows, a.k_rows = x.k_rows;
+  a.where = Packing(x), a.o = x.O, a.lse = x.lse;
   a.part_o = static_cast<float*>(workspace), a.part_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.o_bytes);
-  a.B = x.B, a.max_q = x.max_q, a.max_k = x.max_k, a.hq = x.hq, a.hk = x.hk, a.group = x.hq / x.hk, a.dh = x.dh;
-  a.tiles = p.tiles, a.splits = p.splits, a.chunk = p.chunk;
+  a.B = x.B, a.hq = x.hq, a.hk = x.hk, a.dh = x.dh;
+  a.group = Divisor(x.hq / x.hk), a.splits = Divisor(p.splits), a.tiles = p.tiles, a.chunk = p.chunk;
   a.c = std::max(fabsf(x.scale) * kLog2e, 1e-37f), a.negate = x.scale < 0.f, a.causal = x.causal != 0;
   a.pieces = multiple(x.Q, 16) && multiple(x.K, 16) && multiple(x.V, 16) && x.dh * e % 16 == 0 && x.q_stride * e % 16 == 0 &&
              x.k_stride * e % 16 == 0 && x.v_stride * e % 16 == 0;

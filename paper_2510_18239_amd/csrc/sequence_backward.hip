@@ -17,14 +17,14 @@ namespace {
 struct Args {
   const void *q, *k, *v, *o, *go;
   int64_t q_stride, k_stride, v_stride, dq_stride, dk_stride, dv_stride;  // elements
-  const int32_t *q_offsets, *q_lens, *k_offsets, *k_lens;
+  Packing where;
   const float* lse;
   float *lse2, *delta;  // [hq][q_rows]: lse log2 e, D
   void *dq, *dk, *dv;
-  int64_t q_rows, k_rows;
   float *part_q, *part_kv;  // chunks > 1: [q_splits][q_rows][hq][padded dh], [k_splits][2][k_rows][hk][padded dh]
-  int B, max_q, max_k, hq, hk, group, dh, tiles;
-  int q_splits, q_chunk, k_splits, k_chunk;  // chunks of keys (in keys), and of the steps over queries
+  Divisor group, q_splits, k_splits;
+  int hq, hk, dh, tiles;
+  int q_chunk, k_chunk;  // chunks of keys (in keys), and of the steps over queries
   float scale;
   bool pieces, causal, quads;
 };
@@ -38,18 +38,18 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
   extern __shared__ __align__(1024) unsigned char smem[];  // [2][keys, values]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);
-  const int pairs = a.B * a.hk, pair = blockIdx.x % pairs, rest = blockIdx.x / pairs;
-  const int split = rest % a.q_splits, tile = a.tiles - 1 - rest / a.q_splits;
-  const int b = pair / a.hk, kv = pair % a.hk;
-  const Span qs = span_of(a.q_offsets, a.q_lens, b, a.q_rows, a.max_q), ks = span_of(a.k_offsets, a.k_lens, b, a.k_rows, a.max_k);
-  const int r0 = tile * ROWS, slot_rows = qs.slot * a.group, used_rows = qs.used * a.group;
+  const int kv = blockIdx.x, b = blockIdx.y, group = a.group.d, splits = a.q_splits.d;
+  const int reversed = splits > 1 ? a.q_splits.divide(blockIdx.z) : blockIdx.z, split = blockIdx.z - reversed * splits, tile = a.tiles - 1 - reversed;
+  const auto [qs, ks] = spans_of(a.where, b);
+  const int r0 = tile * ROWS, slot_rows = qs.slot * group, used_rows = qs.used * group;
   if (r0 >= slot_rows) return;
-  const int r = r0 + 32 * wave + n, query = r / a.group, head = kv * a.group + r % a.group;
+  const int r = r0 + 32 * wave + n, query = a.group.divide(r), head = kv * group + r - query * group;
   const bool live = r < used_rows;
-  const int limit = live ? keys_seen(query, qs.used, ks.used, a.causal) : 0;
-  auto last_limit = [&](int rows_end) { return rows_end > 0 ? keys_seen((rows_end - 1) / a.group, qs.used, ks.used, a.causal) : 0; };
+  const int n_q = qs.used, n_k = ks.used;
+  const int limit = live ? keys_seen(query, n_q, n_k, a.causal) : 0;
+  auto last_limit = [&, n_q = n_q, n_k = n_k](int rows_end) { return rows_end > 0 ? keys_seen(a.group.divide(rows_end - 1), n_q, n_k, a.causal) : 0; };
   const int w0 = r0 + 32 * wave, wave_most = w0 < used_rows ? last_limit(min(w0 + 32, used_rows)) : 0;
-  const int wave_least = w0 + 32 <= used_rows ? keys_seen(w0 / a.group, qs.used, ks.used, a.causal) : 0;
+  const int wave_least = w0 + 32 <= used_rows ? keys_seen(a.group.divide(w0), n_q, n_k, a.causal) : 0;
   const int most = r0 < used_rows ? last_limit(min(r0 + ROWS, used_rows)) : 0;
   const int k_begin = split * a.q_chunk, k_end = min(most, k_begin + a.q_chunk), steps = k_end > k_begin ? (k_end - k_begin + KEYS - 1) / KEYS : 0;
 
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
     delta = pair_sum(delta);
   }
   if (live && g == 0 && split == 0) {
-    const int64_t at = head * a.q_rows + qs.start + query;
+    const int64_t at = head * static_cast<int64_t>(a.where.q_rows) + qs.start + query;
     a.lse2[at] = lse2, a.delta[at] = delta;
   }
   f32x16 dq[OB];
@@ -142,8 +142,8 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
     }
   }
   if (r >= slot_rows) return;
-  if (a.q_splits > 1) {
-    float* to = a.part_q + ((split * a.q_rows + qs.start + query) * a.hq + head) * DH;
+  if (splits > 1) {
+    float* to = a.part_q + ((static_cast<int64_t>(split) * a.where.q_rows + qs.start + query) * a.hq + head) * DH;
 #pragma unroll
     for (int ob = 0; ob < OB; ++ob) store_block(to, dq[ob], 1.f, 32 * ob, DH, true, g);
     return;
@@ -164,9 +164,9 @@ __global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);
   // first keys first: under a causal mask most queries see them
-  const int pairs = a.B * a.hk, pair = blockIdx.x % pairs, rest = blockIdx.x / pairs, split = rest % a.k_splits, tile = rest / a.k_splits;
-  const int b = pair / a.hk, kv = pair % a.hk;
-  const Span qs = span_of(a.q_offsets, a.q_lens, b, a.q_rows, a.max_q), ks = span_of(a.k_offsets, a.k_lens, b, a.k_rows, a.max_k);
+  const int kv = blockIdx.x, b = blockIdx.y, group = a.group.d, splits = a.k_splits.d;
+  const int tile = splits > 1 ? a.k_splits.divide(blockIdx.z) : blockIdx.z, split = blockIdx.z - tile * splits;
+  const auto [qs, ks] = spans_of(a.where, b);
   const int j0 = tile * KEYS;
   if (j0 >= ks.slot) return;
   const int key = j0 + 32 * wave + n, shift = ks.used - qs.used;
@@ -176,12 +176,12 @@ __global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
   const int w0 = j0 + 32 * wave, wave_first = w0 < ks.used ? (a.causal ? max(0, w0 - shift) : 0) : qs.used;
   const int wave_all = w0 + 32 <= ks.used ? (a.causal ? max(0, w0 + 31 - shift) : 0) : qs.used;
   const int begin = (a.causal ? max(0, j0 - shift) : 0) / STEP * STEP;
-  const int each = j0 < ks.used && begin < qs.used ? (qs.used - begin + STEP - 1) / STEP : 0, all = each * a.group;
+  const int each = j0 < ks.used && begin < qs.used ? (qs.used - begin + STEP - 1) / STEP : 0, all = each * group;
   const int begin_step = min(all, split * a.k_chunk), steps = min(all - begin_step, a.k_chunk);
 
   const unsigned width = a.dh * sizeof(T);
-  Rows qm{static_cast<const T*>(a.q) + (qs.start + begin) * a.q_stride + kv * a.group * a.dh, static_cast<unsigned>(a.q_stride * sizeof(T)), width, a.pieces};
-  Rows gm{static_cast<const T*>(a.go) + ((qs.start + begin) * a.hq + kv * a.group) * a.dh, static_cast<unsigned>(a.hq * a.dh * sizeof(T)), width, a.pieces};
+  Rows qm{static_cast<const T*>(a.q) + (qs.start + begin) * a.q_stride + kv * group * a.dh, static_cast<unsigned>(a.q_stride * sizeof(T)), width, a.pieces};
+  Rows gm{static_cast<const T*>(a.go) + ((qs.start + begin) * a.hq + kv * group) * a.dh, static_cast<unsigned>(a.hq * a.dh * sizeof(T)), width, a.pieces};
   Loader ql, gl;
   ql.init(qm, tid), gl.init(gm, tid);
   // steps are asked for one head after the other
@@ -193,7 +193,7 @@ __global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
     ql.issue(qm, ask_at, qs.used - begin, to, tid);
     gl.issue(gm, ask_at, qs.used - begin, to + Shape::kBytes, tid);
     if (wave < 2) {
-      const float* from = (wave == 0 ? a.lse2 : a.delta) + (kv * a.group + ask_head) * a.q_rows + qs.start + begin + ask_at;
+      const float* from = (wave == 0 ? a.lse2 : a.delta) + (kv * group + ask_head) * static_cast<int64_t>(a.where.q_rows) + qs.start + begin + ask_at;
       words_to_lds(from, min(count, STEP), reinterpret_cast<float*>(to + 2 * Shape::kBytes) + 64 * wave, lane);
     }
     ask_at += STEP;
@@ -259,8 +259,8 @@ __global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
     }
   }
   if (key >= ks.slot) return;
-  if (a.k_splits > 1) {
-    const int64_t plane = a.k_rows * a.hk * DH;
+  if (splits > 1) {
+    const int64_t plane = static_cast<int64_t>(a.where.k_rows) * a.hk * DH;
     float* to = a.part_kv + 2 * split * plane + ((ks.start + key) * a.hk + kv) * DH;
 #pragma unroll
     for (int ob = 0; ob < OB; ++ob) store_block(to, dk[ob], 1.f, 32 * ob, DH, true, g), store_block(to + plane, dv[ob], 1.f, 32 * ob, DH, true, g);
@@ -279,18 +279,19 @@ __global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void sequence_attention_fold_kernel(Args a, int what, int groups) {
   const Folder<DH> at(groups);
-  const int heads = what == 0 ? a.hq : a.hk, users = a.B, splits = what == 0 ? a.q_splits : a.k_splits;
-  const int b = blockIdx.x % users, i = static_cast<int>(blockIdx.x / users) * at.rows + at.row;
-  const Span span = what == 0 ? span_of(a.q_offsets, a.q_lens, b, a.q_rows, a.max_q) : span_of(a.k_offsets, a.k_lens, b, a.k_rows, a.max_k);
-  const bool live = i / heads < span.slot;
-  const int64_t rows = what == 0 ? a.q_rows : a.k_rows, row = span.start + i / heads, plane = rows * heads * DH;
-  const float* p = (what == 0 ? a.part_q : a.part_kv) + (what == 2 ? plane : 0) + (row * heads + i % heads) * DH;
+  const int heads = what == 0 ? a.hq : a.hk, splits = what == 0 ? a.q_splits.d : a.k_splits.d;
+  const int b = blockIdx.y, head = blockIdx.x, i = blockIdx.z * at.rows + at.row;
+  const Spans spans = spans_of(a.where, b);
+  const Span span = what == 0 ? spans.q : spans.k;
+  const bool live = i < span.slot;
+  const int64_t rows = what == 0 ? a.where.q_rows : a.where.k_rows, row = span.start + i, plane = rows * heads * DH;
+  const float* p = (what == 0 ? a.part_q : a.part_kv) + (what == 2 ? plane : 0) + (row * heads + head) * DH;
   f32x4 sum = at.sum(p, what == 0 ? plane : 2 * plane, splits, groups, live);
   if (!live || at.group != 0) return;
   const float factor = what == 2 ? 1.f : a.scale;
 #pragma unroll
   for (int j = 0; j < 4; ++j) sum[j] *= factor;
-  T* to = static_cast<T*>(what == 0 ? a.dq : what == 1 ? a.dk : a.dv) + row * (what == 0 ? a.dq_stride : what == 1 ? a.dk_stride : a.dv_stride) + i % heads * a.dh;
+  T* to = static_cast<T*>(what == 0 ? a.dq : what == 1 ? a.dk : a.dv) + row * (what == 0 ? a.dq_stride : what == 1 ? a.dk_stride : a.dv_stride) + head * a.dh;
   store_four(to, sum, 4 * at.t, a.dh, a.quads);
 }
 
@@ -323,50 +324,50 @@ Plan plan_of(const SequenceAttention& a) {
 }
 
 template <typename T, int DH>
-hipError_t fold(const Args& a, int what, int most, int heads, int splits, hipStream_t s) {
-  const int groups = fold_groups(splits, DH / 4);
-  const int64_t per = 256 / (DH / 4) / groups, rows = static_cast<int64_t>(most) * heads;
-  hipLaunchKernelGGL((sequence_attention_fold_kernel<T, DH>), dim3(static_cast<unsigned>(a.B * ((rows + per - 1) / per))), dim3(256), 0, s, a, what, groups);
+hipError_t fold(const Args& a, int what, int users, int most, int heads, int splits, hipStream_t s) {
+  const int groups = fold_groups(splits, DH / 4), per = 256 / (DH / 4) / groups;
+  hipLaunchKernelGGL((sequence_attention_fold_kernel<T, DH>), dim3(heads, users, (most + per - 1) / per), dim3(256), 0, s, a, what, groups);
   return hipGetLastError();
 }
 
 template <typename T, int DH>
-hipError_t run(Args a, const Plan& p, hipStream_t s) {
+hipError_t run(Args a, const Plan& p, int users, hipStream_t s) {
   constexpr int STEP = sizeof(T) == 2 ? 64 : 32;
-  const int64_t pairs = static_cast<int64_t>(a.B) * a.hk;
-  if (a.max_q > 0) {
+  const int max_q = a.where.max_q, max_k = a.where.max_k;
+  if (max_q > 0) {
     constexpr int lds = 4 * Tile<T, DH, STEP>::kBytes;
     static PerDevice granted;
     const auto kernel = sequence_attention_dq_kernel<T, DH, 4, STEP>;
     if (hipError_t e = allow_lds(granted, reinterpret_cast<const void*>(kernel), lds); e != hipSuccess) return e;
     a.tiles = p.q_tiles;
-    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(pairs * p.q_tiles * p.q_splits)), dim3(256), lds, s, a);
+    hipLaunchKernelGGL(kernel, dim3(a.hk, users, p.q_tiles * p.q_splits), dim3(256), lds, s, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (p.q_splits > 1)
-      if (hipError_t e = fold<T, DH>(a, 0, a.max_q, a.hq, p.q_splits, s); e != hipSuccess) return e;
+      if (hipError_t e = fold<T, DH>(a, 0, users, max_q, a.hq, p.q_splits, s); e != hipSuccess) return e;
   }
-  if (a.max_k == 0) return hipSuccess;
+  if (max_k == 0) return hipSuccess;
   constexpr int lds = 2 * (2 * Tile<T, DH, STEP>::kBytes + 512);
   static PerDevice granted;
   const auto kernel = sequence_attention_dkv_kernel<T, DH, STEP>;
   if (hipError_t e = allow_lds(granted, reinterpret_cast<const void*>(kernel), lds); e != hipSuccess) return e;
-  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(pairs * p.k_tiles * p.k_splits)), dim3(256), lds, s, a);
+  hipLaunchKernelGGL(kernel, dim3(a.hk, users, p.k_tiles * p.k_splits), dim3(256), lds, s, a);
   if (hipError_t e = hipGetLastError(); e != hipSuccess || p.k_splits == 1) return e;
-  if (hipError_t e = fold<T, DH>(a, 1, a.max_k, a.hk, p.k_splits, s); e != hipSuccess) return e;
-  return fold<T, DH>(a, 2, a.max_k, a.hk, p.k_splits, s);
+  if (hipError_t e = fold<T, DH>(a, 1, users, max_k, a.hk, p.k_splits, s); e != hipSuccess) return e;
+  return fold<T, DH>(a, 2, users, max_k, a.hk, p.k_splits, s);
 }
 
 bool multiple(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
 }  // namespace
 
-bool sequence_attention_backward_fits(const SequenceAttention& a) {  // 2^32 work items a launch
+bool sequence_attention_backward_fits(const SequenceAttention& a) {  // 2^32 work items a launch, 65535 workgroups along the grid's third axis
   const int64_t rows = static_cast<int64_t>(a.max_q) * (a.hq / a.hk), pairs = static_cast<int64_t>(a.B) * a.hk;
   if (rows >= (int64_t{1} << 31) - 128 || pairs >= (int64_t{1} << 24)) return false;
   const Plan p = plan_of(a);
-  return pairs * p.q_tiles * p.q_splits < (int64_t{1} << 24) && pairs * p.k_tiles * p.k_splits < (int64_t{1} << 24) &&
-         (p.q_splits == 1 || a.B * static_cast<int64_t>(a.max_q) * a.hq < (int64_t{1} << 24)) &&
-         (p.k_splits == 1 || a.B * static_cast<int64_t>(a.max_k) * a.hk < (int64_t{1} << 24));
+  const int64_t q_deep = static_cast<int64_t>(p.q_tiles) * p.q_splits, k_deep = static_cast<int64_t>(p.k_tiles) * p.k_splits;
+  auto folds = [&](int most, int heads) { return most < 65536 && a.B * static_cast<int64_t>(most) * heads < (int64_t{1} << 24); };
+  return q_deep < 65536 && k_deep < 65536 && pairs * q_deep < (int64_t{1} << 24) && pairs * k_deep < (int64_t{1} << 24) &&
+         (p.q_splits == 1 || folds(a.max_q, a.hq)) && (p.k_splits == 1 || folds(a.max_k, a.hk));
 }
 
 size_t sequence_attention_backward_workspace(const SequenceAttention& a) { return plan_of(a).bytes; }
@@ -378,21 +379,21 @@ hipError_t sequence_attention_backward(const SequenceAttention& x, void* workspa
   a.q = x.Q, a.k = x.K, a.v = x.V, a.o = x.O, a.go = x.dO, a.dq = x.dQ, a.dk = x.dK, a.dv = x.dV, a.lse = x.lse;
   a.q_stride = x.q_stride, a.k_stride = x.k_stride, a.v_stride = x.v_stride;
   a.dq_stride = x.dq_stride, a.dk_stride = x.dk_stride, a.dv_stride = x.dv_stride;
-  a.q_offsets = x.q_offsets, a.q_lens = x.q_lens, a.k_offsets = x.k_offsets, a.k_lens = x.k_lens;
+  a.where = Packing(x);
   char* at = static_cast<char*>(workspace);
   a.lse2 = reinterpret_cast<float*>(at), at += p.stats;
   a.delta = reinterpret_cast<float*>(at), at += p.stats;
   a.part_q = reinterpret_cast<float*>(at), at += p.part_q;
   a.part_kv = reinterpret_cast<float*>(at);
-  a.q_splits = p.q_splits, a.q_chunk = p.q_chunk, a.k_splits = p.k_splits, a.k_chunk = p.k_chunk;
-  a.q_rows = x.q_rows, a.k_rows = x.k_rows, a.B = x.B, a.max_q = x.max_q, a.max_k = x.max_k, a.hq = x.hq, a.hk = x.hk, a.group = x.hq / x.hk, a.dh = x.dh;
+  a.group = Divisor(x.hq / x.hk), a.q_splits = Divisor(p.q_splits), a.q_chunk = p.q_chunk, a.k_splits = Divisor(p.k_splits), a.k_chunk = p.k_chunk;
+  a.hq = x.hq, a.hk = x.hk, a.dh = x.dh;
   a.scale = x.scale, a.causal = x.causal != 0;
   a.pieces = multiple(x.Q, 16) && multiple(x.K, 16) && multiple(x.V, 16) && multiple(x.O, 16) && multiple(x.dO, 16) && x.dh * e % 16 == 0 &&
              x.q_stride * e % 16 == 0 && x.k_stride * e % 16 == 0 && x.v_stride * e % 16 == 0;
   a.quads = x.dh % 4 == 0 && x.dq_stride % 4 == 0 && x.dk_stride % 4 == 0 && x.dv_stride % 4 == 0 && multiple(x.dQ, 4 * e) && multiple(x.dK, 4 * e) &&
             multiple(x.dV, 4 * e);
-  if (x.dtype == 1) return p.dh == 32 ? run<bf16_t, 32>(a, p, s) : p.dh == 64 ? run<bf16_t, 64>(a, p, s) : run<bf16_t, 128>(a, p, s);
-  return p.dh == 32 ? run<float, 32>(a, p, s) : p.dh == 64 ? run<float, 64>(a, p, s) : run<float, 128>(a, p, s);
+  if (x.dtype == 1) return p.dh == 32 ? run<bf16_t, 32>(a, p, x.B, s) : p.dh == 64 ? run<bf16_t, 64>(a, p, x.B, s) : run<bf16_t, 128>(a, p, x.B, s);
+  return p.dh == 32 ? run<float, 32>(a, p, x.B, s) : p.dh == 64 ? run<float, 64>(a, p, x.B, s) : run<float, 128>(a, p, x.B, s);
 }
 
 }  // namespace lime

@@ -1,6 +1,7 @@
 // What the forward and the backward pass of the attention over packed sequences share on the device.
 #pragma once
 
+#include "divisor.hpp"
 #include "encoder.hpp"
 #include "tiles.hpp"
 
@@ -8,20 +9,39 @@ namespace lime {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
+// Which rows of the packed tensors are whose.  Lengths that are not given point at the offsets, so that they can be read along.
+struct Packing {
+  const int32_t *q_offsets, *q_lens, *k_offsets, *k_lens;
+  int q_rows, k_rows, max_q, max_k;
+  bool has_q_lens, has_k_lens;
+  Packing() = default;
+  explicit Packing(const SequenceAttention& x)
+      : q_offsets(x.q_offsets), q_lens(x.q_lens ? x.q_lens : x.q_offsets), k_offsets(x.k_offsets), k_lens(x.k_lens ? x.k_lens : x.k_offsets),
+        q_rows(static_cast<int>(x.q_rows)), k_rows(static_cast<int>(x.k_rows)), max_q(x.max_q), max_k(x.max_k), has_q_lens(x.q_lens != nullptr),
+        has_k_lens(x.k_lens != nullptr) {}
+};
+
 // A user's slot of a packed tensor and the rows of it that are in use.  Offsets and lengths are cut to the tensor, so that
 // what they hold never takes an access outside it.
 struct Span {
   int64_t start;
   int slot, used;
 };
-__device__ __forceinline__ Span span_of(const int32_t* offsets, const int32_t* lens, int b, int64_t rows, int most) {
-  const int64_t start = min(max(static_cast<int64_t>(offsets[b]), int64_t{0}), rows);
-  const int64_t end = min(max(static_cast<int64_t>(offsets[b + 1]), start), rows);
-  const int slot = static_cast<int>(min(end - start, static_cast<int64_t>(most)));
-  return {start, slot, lens ? min(max(lens[b], 0), slot) : slot};
+struct Spans {
+  Span q, k;
+};
+__device__ __forceinline__ Spans spans_of(const Packing& p, int b) {
+  // all of them asked for before any is looked at: one wait of a kernel's start instead of four
+  const int q0 = p.q_offsets[b], q1 = p.q_offsets[b + 1], k0 = p.k_offsets[b], k1 = p.k_offsets[b + 1], ql = p.q_lens[b], kl = p.k_lens[b];
+  auto span = [](int begin, int end, int len, bool has, int rows, int most) -> Span {
+    begin = min(max(begin, 0), rows), end = min(max(end, begin), rows);
+    const int slot = min(end - begin, most);
+    return {begin, slot, has ? min(max(len, 0), slot) : slot};
+  };
+  return {span(q0, q1, ql, p.has_q_lens, p.q_rows, p.max_q), span(k0, k1, kl, p.has_k_lens, p.k_rows, p.max_k)};
 }
 
 // How many keys query i of a user sees: all, or those up to its own place counted from the end.
-__device__ __forceinline__ int keys_seen(int i, int n_q, int n_k, int causal) { return causal ? min(n_k, max(0, i + 1 + n_k - n_q)) : n_k; }
+__device__ __forceinline__ int keys_seen(int i, int n_q, int n_k, bool causal) { return causal ? min(n_k, max(0, i + 1 + n_k - n_q)) : n_k; }
 
 }  // namespace lime
