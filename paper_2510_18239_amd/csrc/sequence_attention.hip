@@ -29,14 +29,14 @@ struct Args {
 // this (a factor of 2^8 in p, which neither fp32 sums nor the rounding of p mind): rarely after a row's first tiles.
 constexpr float kHeadroom = 8.f;
 
-// WAVES waves of 32 rows each; KEYS keys a step, STAGES steps' tiles in LDS (one in use, the others on their way).
-template <typename T, int DH, int WAVES, int KEYS, int STAGES>
+// WAVES waves of 32 rows each; KEYS keys a step, two steps' tiles in LDS (one in use, the other on its way).
+template <typename T, int DH, int WAVES, int KEYS>
 __global__ __launch_bounds__(WAVES * 64) void sequence_attention_kernel(Args a) {
   using Shape = Tile<T, DH, KEYS>;
   using Loader = TileLoader<T, DH, KEYS, WAVES>;
   using Reader = TileReader<T, DH, KEYS>;
   constexpr int KB = KEYS / 32, OB = DH / 32, NK = DH / 16, ROWS = 32 * WAVES;
-  extern __shared__ __align__(1024) unsigned char smem[];  // [STAGES][keys, values]
+  extern __shared__ __align__(1024) unsigned char smem[];  // [2][keys, values]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);
   // key heads and users fastest: the workgroups of one of them, which read the same keys, land on the same XCD where their number
@@ -65,14 +65,12 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_kernel(Args a) 
   const Rows km{kp, static_cast<unsigned>(a.k_stride * sizeof(T)), width, a.pieces}, vm{vp, static_cast<unsigned>(a.v_stride * sizeof(T)), width, a.pieces};
   Loader kl, vl;
   kl.init(km, tid), vl.init(vm, tid);
-  auto stage = [&](int i) { return smem + (i % STAGES) * 2 * Shape::kBytes; };
+  auto stage = [&](int i) { return smem + i % 2 * 2 * Shape::kBytes; };
   auto ask = [&](int i) {
     kl.issue(km, i * KEYS, k_end - k_begin, stage(i), tid);
     vl.issue(vm, i * KEYS, k_end - k_begin, stage(i) + Shape::kBytes, tid);
   };
-#pragma unroll
-  for (int i = 0; i < STAGES - 1; ++i)
-    if (i < steps) ask(i);
+  if (steps > 0) ask(0);
 
   Fragment<T> q[NK];
   const T* qp = static_cast<const T*>(a.q) + (qs.start + query) * a.q_stride + head * a.dh;
@@ -87,10 +85,9 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_kernel(Args a) 
   float m = -INFINITY, l = 0.f;  // of this lane's row; l of the lane half's keys
 
   for (int i = 0; i < steps; ++i) {
-    if (STAGES > 2 && i + STAGES - 1 <= steps) wait_lds_loads<(STAGES - 2) * 2 * Loader::kLoads>();
-    else wait_lds_loads<0>();
+    wait_lds_loads<0>();
     lds_barrier();  // everyone's part of this step's tiles is there, and everyone is done with the last step's
-    if (i + STAGES - 1 < steps) ask(i + STAGES - 1);
+    if (i + 1 < steps) ask(i + 1);
     const int key0 = k_begin + i * KEYS;
     if (key0 >= wave_most) continue;
     const unsigned char *kt = stage(i), *vt = kt + Shape::kBytes;
@@ -209,7 +206,10 @@ struct Plan {
 };
 
 // Rows that one wave holds take a workgroup of one wave.  Where the tiles of rows are too few to fill the chip, the keys are cut
-// into chunks as well, none shorter than 256 keys.
+// into chunks as well.  A lone wave needs about 1600 cycles for a step of 32 keys, most of them waiting for itself, and 4600 to start
+// and to end: so eight waves a compute unit are wanted, of four steps at least, but no more than 256 chunks of a row, which have to be
+// folded again.  (32 users, up to 4096 keys: 14.6 us in chunks of 128 keys, 15.8 of 256; four users of up to 131072: 53 us in 512 chunks,
+// 49 in 256.  More tiles in flight take the LDS of the other waves: three 16.0, four 15.7 and 51.9.)
 Plan plan_of(const SequenceAttention& a) {
   const int64_t B = a.B, hk = a.hk, max_k = std::max(a.max_k, 1), rows = std::max<int64_t>(a.max_q, 1) * (a.hq / a.hk);
   const int dh = a.dh, dtype = a.dtype;
@@ -219,8 +219,9 @@ Plan plan_of(const SequenceAttention& a) {
   p.keys = dtype == 1 && p.waves > 1 ? 64 : 32;
   p.tiles = static_cast<int>((rows + 32 * p.waves - 1) / (32 * p.waves));
   const int64_t groups = B * hk * p.tiles;
-  const int64_t want = (p.waves == 1 ? 4 : 2) * static_cast<int64_t>(compute_units());
-  int64_t splits = groups >= want ? 1 : std::min((want + groups - 1) / groups, (max_k + 255) / 256);
+  const int64_t want = (p.waves == 1 ? 8 : 2) * static_cast<int64_t>(compute_units());
+  const int64_t least = p.waves == 1 ? std::max<int64_t>(128, (max_k + 255) / 256) : 256;
+  int64_t splits = groups >= want ? 1 : std::min((want + groups - 1) / groups, (max_k + least - 1) / least);
   int64_t chunk = (max_k + splits - 1) / splits;
   chunk = (chunk + p.keys - 1) / p.keys * p.keys;
   splits = (max_k + chunk - 1) / chunk;
@@ -233,11 +234,11 @@ Plan plan_of(const SequenceAttention& a) {
   return p;
 }
 
-template <typename T, int DH, int WAVES, int KEYS, int STAGES>
+template <typename T, int DH, int WAVES, int KEYS>
 hipError_t launch(const Args& a, hipStream_t s) {
-  constexpr int lds = STAGES * 2 * Tile<T, DH, KEYS>::kBytes;
+  constexpr int lds = 4 * Tile<T, DH, KEYS>::kBytes;
   static PerDevice granted;
-  const auto kernel = sequence_attention_kernel<T, DH, WAVES, KEYS, STAGES>;
+  const auto kernel = sequence_attention_kernel<T, DH, WAVES, KEYS>;
   if (hipError_t e = allow_lds(granted, reinterpret_cast<const void*>(kernel), lds); e != hipSuccess) return e;
   hipLaunchKernelGGL(kernel, dim3(a.hk, a.B, a.tiles * a.splits.d), dim3(WAVES * 64), lds, s, a);
   return hipGetLastError();
@@ -246,7 +247,7 @@ hipError_t launch(const Args& a, hipStream_t s) {
 template <typename T, int DH>
 hipError_t run(const Args& a, const Plan& p, hipStream_t s) {
   constexpr int KEYS = sizeof(T) == 2 ? 64 : 32;
-  hipError_t e = p.waves == 1 ? launch<T, DH, 1, 32, sizeof(T) == 2 ? 4 : 2>(a, s) : launch<T, DH, 4, KEYS, 2>(a, s);
+  hipError_t e = p.waves == 1 ? launch<T, DH, 1, 32>(a, s) : launch<T, DH, 4, KEYS>(a, s);
   if (e != hipSuccess || a.splits.d == 1) return e;
   const int groups = fold_groups(a.splits.d, DH / 4);
   const int64_t rows = static_cast<int64_t>(a.where.max_q) * a.group.d, per = 256 / (DH / 4) / groups;

@@ -171,6 +171,8 @@ struct Rows {
 
 // Fills tiles by WAVES waves, 1 KiB a load, from memory straight to LDS.  Rows at or past the given count and columns past the
 // width come out as zeros: the loads go through a buffer whose size ends with the last row, and what lies outside reads as zero.
+// (The loads are not said to touch memory, so that the compiler may work on other tiles among them; who fills a tile has passed a
+// barrier since its last use, and who reads it waits and passes one, and those are.)
 template <typename T, int DH, int ROWS, int WAVES>
 struct TileLoader {
   using Shape = Tile<T, DH, ROWS>;
@@ -208,8 +210,7 @@ struct TileLoader {
         unsigned at_row;  // (added here, not by the compiler: it would keep all the sums in registers across the kernel's loop)
         asm volatile("s_mov_b32 m0, %1\n\tv_add_u32_e32 %0, %2, %3\n\tbuffer_load_dwordx4 %0, %4, 0 offen lds"
                      : "=&v"(at_row)
-                     : "s"(lds + WAVES * 1024 * i), "s"(i / kOffsets * kOffsets * kRowsALoad * m.stride), "v"(offset[i % kOffsets]), "s"(resource)
-                     : "memory");
+                     : "s"(lds + WAVES * 1024 * i), "s"(i / kOffsets * kOffsets * kRowsALoad * m.stride), "v"(offset[i % kOffsets]), "s"(resource));
       }
     } else {
       const unsigned columns = m.width / sizeof(T);
@@ -232,7 +233,7 @@ __device__ __forceinline__ void words_to_lds(const void* from, int count, void* 
   resource[2] = __builtin_amdgcn_readfirstlane(count * 4u);
   resource[3] = 0x00020000u;
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
-               : : "s"(__builtin_amdgcn_readfirstlane(lds_offset_of(to))), "v"(lane * 4u), "s"(resource) : "memory");
+               : : "s"(__builtin_amdgcn_readfirstlane(lds_offset_of(to))), "v"(lane * 4u), "s"(resource));
 }
 
 // The 16-deep fragments of one row of `width` bytes, straight from memory: lane half g's slots hold columns 16 kk + 8g .. + 7.
