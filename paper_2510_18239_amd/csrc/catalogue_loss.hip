@@ -148,7 +148,7 @@ __global__ __launch_bounds__(256) void catalogue_lse_kernel(Args a) {
     wait_lds_loads<0>();
     lds_barrier();
     if (i + 1 < steps) wl.issue(wm, (i + 1) * STEP, v1 - v0, smem + (i + 1) % 2 * Shape::kBytes, tid);
-    const unsigned char* wt = smem + i % 2 * Shape::kBytes;
+    const unsigned wt = lds_offset_of(smem + i % 2 * Shape::kBytes);
     f32x16 s[VB];
 #pragma unroll
     for (int vb = 0; vb < VB; ++vb) {
@@ -245,7 +245,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void catalogue_dx_kern
     wait_lds_loads<0>();
     lds_barrier();
     if (i + 1 < steps) wl.issue(wm, (i + 1) * STEP, v1 - v0, smem + (i + 1) % 2 * Shape::kBytes, tid);
-    const unsigned char* wt = smem + i % 2 * Shape::kBytes;
+    const unsigned wt = lds_offset_of(smem + i % 2 * Shape::kBytes);
 #pragma unroll
     for (int vb = 0; vb < VB; ++vb) {
       f32x16 p = zero_block();
@@ -324,8 +324,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void catalogue_dw_kern
     wait_lds_loads<0>();
     lds_barrier();
     if (i + 1 < steps) ask(i + 1);
-    const unsigned char* xt = smem + i % 2 * kStage;
-    const float *lse2 = reinterpret_cast<const float*>(xt + Shape::kBytes), *weight = lse2 + 64;
+    const unsigned char* rows = smem + i % 2 * kStage;
+    const unsigned xt = lds_offset_of(rows);
+    const float *lse2 = reinterpret_cast<const float*>(rows + Shape::kBytes), *weight = lse2 + 64;
     const int32_t* target = reinterpret_cast<const int32_t*>(weight + 64);
     const float* own = weight + 128;
     // which of the step's rows have one of the wave's items for their target (rows past the last: with the weight 0)

@@ -90,7 +90,7 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_kernel(Args a) 
     if (i + 1 < steps) ask(i + 1);
     const int key0 = k_begin + i * KEYS;
     if (key0 >= wave_most) continue;
-    const unsigned char *kt = stage(i), *vt = kt + Shape::kBytes;
+    const unsigned kt = lds_offset_of(stage(i)), vt = kt + Shape::kBytes;
     f32x16 s[KB];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {

@@ -80,12 +80,12 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
     wait_lds_loads<0>();
     lds_barrier();
     for (int kb = 0; kb < KB * steps; ++kb) {
-      const unsigned char *kt = smem + kb / KB * 2 * Shape::kBytes, *vt = kt + Shape::kBytes;
+      const unsigned kt = lds_offset_of(smem + kb / KB * 2 * Shape::kBytes) + kb % KB * 32 * Shape::kRowBytes, vt = kt + Shape::kBytes;
       f32x16 s = zero_block(), e = zero_block();
 #pragma unroll
       for (int kk = 0; kk < NK; ++kk) {
-        s = mma16(read.row(kt, kb % KB * 32, kk), q[kk], s);
-        e = mma16(read.row(vt, kb % KB * 32, kk), go[kk], e);
+        s = mma16(read.row(kt, 0, kk), q[kk], s);
+        e = mma16(read.row(vt, 0, kk), go[kk], e);
       }
 #pragma unroll
       for (int x = 0; x < 16; ++x)
@@ -115,7 +115,7 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
     if (i + 1 < steps && !resident) ask(i + 1);
     const int key0 = k_begin + i * KEYS;
     if (key0 >= wave_most) continue;
-    const unsigned char *kt = smem + i % 2 * 2 * Shape::kBytes, *vt = kt + Shape::kBytes;
+    const unsigned kt = lds_offset_of(smem + i % 2 * 2 * Shape::kBytes), vt = kt + Shape::kBytes;
     const bool partial = key0 + KEYS > wave_least;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
@@ -219,8 +219,9 @@ __global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
     const int q0 = begin + at;
     at = at + STEP < each * STEP ? at + STEP : 0;
     if (q0 + STEP <= wave_first) continue;
-    const unsigned char *qt = smem + i % 2 * kStage, *gt = qt + Shape::kBytes;
-    const float *lse2 = reinterpret_cast<const float*>(gt + Shape::kBytes), *delta = lse2 + 64;
+    const unsigned char* tiles = smem + i % 2 * kStage;
+    const unsigned qt = lds_offset_of(tiles), gt = qt + Shape::kBytes;
+    const float *lse2 = reinterpret_cast<const float*>(tiles + 2 * Shape::kBytes), *delta = lse2 + 64;
     const bool partial = q0 < wave_all || q0 + STEP > qs.used;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {

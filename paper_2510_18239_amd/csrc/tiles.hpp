@@ -93,71 +93,74 @@ struct Tile {
   static constexpr int kRowBytes = DH * static_cast<int>(sizeof(T)), kPieces = kRowBytes / 16, kBytes = ROWS * kRowBytes;
   static constexpr int kPerPiece = 16 / static_cast<int>(sizeof(T));
   static_assert(DH % 32 == 0 && ROWS % 16 == 0);
-  // Which piece sits in slot s of row r: s ^ swizzle(r).  Eight consecutive rows read at one column (a row fragment) and four
-  // rows at two neighbouring pieces (what sixteen lanes read for a column fragment) fall on different banks.
+  // Which piece sits in slot s of row r: s ^ swizzle(r).  The 64 banks serve 256 bytes at a time: sixteen consecutive rows at one piece
+  // (a row fragment) and four consecutive rows at four neighbouring pieces (half a wave's part of a column fragment).  Either falls on
+  // 16 different slots of the 256 bytes, which hold one, two or four rows.  (Laid out for 128 bytes, half of the cycles were conflicts.)
   __device__ static constexpr int swizzle(int r) {
-    return kPieces >= 8 ? ((r & 3) << 1) | ((r >> 2) & 1) : (((r >> 1) & 1) << 1) | ((r >> 2) & 1);
+    return kPieces >= 16 ? ((r & 3) << 2) | ((r >> 2) & 3) : kPieces == 8 ? (((r >> 1) & 1) << 2) | ((r >> 2) & 3) : (r >> 2) & 3;
   }
 };
 
-// Where a lane's fragments begin in a tile.  The swizzle stays within 128 bytes, so that a few places and the instructions' own
-// offsets reach all of them (with a place of its own for each fragment, the widest kernels had no registers left).
+// Where a lane's fragments lie in a tile (at an LDS offset that is a multiple of 256).  The swizzle is an exclusive or, so that one place
+// a kind of fragment gives all of them: another column is another bit of the place, another sixteen rows an offset of the instruction.
+// (With a place of its own for each fragment, the widest kernels had no registers left.)
 template <typename T, int DH, int ROWS>
 class TileReader {
   using Shape = Tile<T, DH, ROWS>;
-  static constexpr int kSpan = Shape::kRowBytes < 128 ? Shape::kRowBytes : 128;  // bytes of a row that the swizzle permutes
-  static constexpr int kStep = 16 * static_cast<int>(sizeof(T));                 // bytes of 16 columns
-  static constexpr int kKs = kSpan / kStep;                                      // 16-column steps within a span
-  unsigned row_[kKs];
-  unsigned column_[sizeof(T) == 2 ? 2 : 4];
+  static constexpr int kSpan = Shape::kRowBytes < 256 ? Shape::kRowBytes : 256;  // bytes of a row that the swizzle permutes
+  unsigned row_, column_;
+
+  template <typename V>
+  __device__ static V at(unsigned place) {
+    return *reinterpret_cast<__attribute__((address_space(3))) const V*>(place);
+  }
+  // `place` moved by `bytes` along its row
+  __device__ static unsigned along(unsigned place, int bytes) { return (place ^ (bytes % kSpan)) + bytes / kSpan * kSpan; }
 
  public:
   __device__ explicit TileReader(int lane) {
     const int n = lane & 31, g = lane >> 5;
-#pragma unroll
-    for (int kk = 0; kk < kKs; ++kk) row_[kk] = n * Shape::kRowBytes + ((kStep / 16 * kk + kStep / 32 * g) ^ Shape::swizzle(n)) * 16;
+    row_ = n * Shape::kRowBytes + ((static_cast<int>(sizeof(T)) / 2 * g) ^ Shape::swizzle(n)) * 16;
     if constexpr (sizeof(T) == 2) {
       // ds_read_b64_tr_b16: each lane of a group of 16 gets a column of the 4 x 16 block whose rows the group's lanes point
       // at, four lanes a row
       const int r = 4 * g + (lane & 15) / 4, piece = 2 * ((lane >> 4) & 1) + (lane & 3) / 2;
-#pragma unroll
-      for (int odd = 0; odd < 2; ++odd)
-        column_[odd] = r * Shape::kRowBytes + ((piece + (kSpan == 128 ? 4 * odd : 0)) ^ Shape::swizzle(r)) * 16 + (lane & 1) * 8;
+      column_ = r * Shape::kRowBytes + (piece ^ Shape::swizzle(r)) * 16 + (lane & 1) * 8;
     } else {
-#pragma unroll
-      for (int t = 0; t < 4; ++t) column_[t] = (4 * g + t) * Shape::kRowBytes + ((n / 4) ^ Shape::swizzle(4 * g + t)) * 16 + (n & 3) * 4;
+      column_ = 4 * g * Shape::kRowBytes + ((n / 4) ^ Shape::swizzle(4 * g)) * 16 + (n & 3) * 4;
     }
   }
   // r0 a multiple of 32
-  __device__ Fragment<T> row(const unsigned char* tile, int r0, int kk) const {
-    const unsigned char* at = tile + row_[kk % kKs] + (r0 * Shape::kRowBytes + kk / kKs * 128);
+  __device__ Fragment<T> row(unsigned tile, int r0, int kk) const {
+    const unsigned place = along(tile + row_, 16 * kk * static_cast<int>(sizeof(T))) + r0 * Shape::kRowBytes;
     if constexpr (sizeof(T) == 2) {
-      return *reinterpret_cast<const bf16x8*>(at);
+      return at<bf16x8>(place);
     } else {
-      const f32x4 lo = *reinterpret_cast<const f32x4*>(at);
-      const f32x4 hi = *reinterpret_cast<const f32x4*>(tile + (row_[kk % kKs] ^ 16u) + (r0 * Shape::kRowBytes + kk / kKs * 128));
+      const f32x4 lo = at<f32x4>(place), hi = at<f32x4>(place ^ 16u);
       return in_parts(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
   }
   // r0 a multiple of 16, c0 of 32
-  __device__ Fragment<T> column(const unsigned char* tile, int r0, int c0) const {
+  __device__ Fragment<T> column(unsigned tile, int r0, int c0) const {
+    const unsigned place = along(tile + column_, c0 * static_cast<int>(sizeof(T)));
     if constexpr (sizeof(T) == 2) {
-      const int ob = c0 / 32;
-      const unsigned char* at = tile + column_[ob % 2] + (r0 * Shape::kRowBytes + ob / 2 * 128);
-      // (eight rows on, the swizzle is the same)
-      const bf16x4 lo = transposed(at), hi = transposed(at + 8 * Shape::kRowBytes);
+      const bf16x4 lo = transposed(place + r0 * Shape::kRowBytes);
+      const bf16x4 hi = transposed((place ^ (Shape::swizzle(8) * 16u)) + (r0 + 8) * Shape::kRowBytes);  // eight rows on
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
       f32x8 v;
 #pragma unroll
-      for (int t = 0; t < 8; ++t) v[t] = *reinterpret_cast<const float*>(tile + column_[t & 3] + ((r0 + t / 4 * 8) * Shape::kRowBytes + c0 * 4));
+      for (int t = 0; t < 8; ++t) {
+        const int r = chain_k(0, t);
+        v[t] = at<float>((place ^ (Shape::swizzle(r) * 16u)) + (r0 + r) * Shape::kRowBytes);
+      }
       return in_parts(v);
     }
   }
 
  private:
-  __device__ static bf16x4 transposed(const unsigned char* q) {
-    return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(q)));
+  __device__ static bf16x4 transposed(unsigned place) {
+    return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<__attribute__((address_space(3))) s16x4*>(place)));
   }
 };
 
@@ -179,7 +182,7 @@ struct TileLoader {
   static constexpr int kLoads = Shape::kBytes / 1024 / WAVES;  // a wave's, for one tile
   static_assert(kLoads * WAVES * 1024 == Shape::kBytes && ROWS <= 128);
   static constexpr int kRowsALoad = WAVES * 1024 / Shape::kRowBytes;               // from one of a wave's loads to its next
-  static constexpr int kOffsets = kRowsALoad >= 8 ? 1 : 8 / kRowsALoad < kLoads ? 8 / kRowsALoad : kLoads;  // the swizzle repeats after eight rows
+  static constexpr int kOffsets = kRowsALoad >= 16 ? 1 : 16 / kRowsALoad < kLoads ? 16 / kRowsALoad : kLoads;  // the swizzle repeats after 16 rows
   unsigned offset[kOffsets];
 
   __device__ void init(const Rows& m, int tid) {
