@@ -16,6 +16,7 @@ struct Args {
   const void *q, *k, *v;
   int64_t q_stride, k_stride, v_stride;  // elements
   Packing where;
+  Deal deal;
   void* o;
   float* lse;
   float *part_o, *part_ml;  // splits > 1: [splits][B][hk][max_q group][padded dh], [...][2]
@@ -39,9 +40,9 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_kernel(Args a) 
   extern __shared__ __align__(1024) unsigned char smem[];  // [2][keys, values]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);
-  // key heads and users fastest: the workgroups of one of them, which read the same keys, land on the same XCD where their number
-  // is a multiple of eight; last tiles of rows first, under a causal mask the longest
-  const int kv = blockIdx.x, b = blockIdx.y, pairs = a.B * a.hk, pair = b * a.hk + kv, group = a.group.d, splits = a.splits.d;
+  // last tiles of rows first: under a causal mask the longest
+  const auto [b, kv, pair] = pair_of(a.deal);
+  const int pairs = a.deal.pairs.d, group = a.group.d, splits = a.splits.d;
   const int reversed = splits > 1 ? a.splits.divide(blockIdx.z) : blockIdx.z, split = blockIdx.z - reversed * splits, tile = a.tiles - 1 - reversed;
   const auto [qs, ks] = spans_of(a.where, b);
   const int r0 = tile * ROWS, slot_rows = qs.slot * group, used_rows = qs.used * group;
@@ -160,7 +161,7 @@ __global__ __launch_bounds__(256) void sequence_attention_merge_kernel(Args a, i
   __shared__ f32x4 met[256];
   __shared__ float met_m[256], met_l[256];
   const Folder<DH> at(groups);
-  const int kv = blockIdx.x, b = blockIdx.y, pairs = a.B * a.hk, pair = b * a.hk + kv, group = a.group.d, splits = a.splits.d;
+  const int kv = blockIdx.x, b = blockIdx.y, pairs = a.deal.pairs.d, pair = b * a.hk + kv, group = a.group.d, splits = a.splits.d;
   const int r = blockIdx.z * at.rows + at.row;
   const Span qs = spans_of(a.where, b).q;
   const bool live = r < qs.slot * group;
@@ -274,7 +275,7 @@ hipError_t sequence_attention(const SequenceAttention& x, void* workspace, hipSt
   const size_t e = x.dtype == 1 ? 2 : 4;
   Args a{};
   a.q = x.Q, a.k = x.K, a.v = x.V, a.q_stride = x.q_stride, a.k_stride = x.k_stride, a.v_stride = x.v_stride;
-  a.where = Packing(x), a.o = x.O, a.lse = x.lse;
+  a.where = Packing(x), a.deal = Deal(x, p.splits), a.o = x.O, a.lse = x.lse;
   a.part_o = static_cast<float*>(workspace), a.part_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.o_bytes);
   a.B = x.B, a.hq = x.hq, a.hk = x.hk, a.dh = x.dh;
   a.group = Divisor(x.hq / x.hk), a.splits = Divisor(p.splits), a.tiles = p.tiles, a.chunk = p.chunk;

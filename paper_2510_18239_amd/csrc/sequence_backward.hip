@@ -18,6 +18,7 @@ struct Args {
   const void *q, *k, *v, *o, *go;
   int64_t q_stride, k_stride, v_stride, dq_stride, dk_stride, dv_stride;  // elements
   Packing where;
+  Deal deal;
   const float* lse;
   float *lse2, *delta;  // [hq][q_rows]: lse log2 e, D
   void *dq, *dk, *dv;
@@ -38,7 +39,8 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
   extern __shared__ __align__(1024) unsigned char smem[];  // [2][keys, values]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);
-  const int kv = blockIdx.x, b = blockIdx.y, group = a.group.d, splits = a.q_splits.d;
+  const auto [b, kv, pair] = pair_of(a.deal);
+  const int group = a.group.d, splits = a.q_splits.d;
   const int reversed = splits > 1 ? a.q_splits.divide(blockIdx.z) : blockIdx.z, split = blockIdx.z - reversed * splits, tile = a.tiles - 1 - reversed;
   const auto [qs, ks] = spans_of(a.where, b);
   const int r0 = tile * ROWS, slot_rows = qs.slot * group, used_rows = qs.used * group;
@@ -164,7 +166,8 @@ __global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);
   // first keys first: under a causal mask most queries see them
-  const int kv = blockIdx.x, b = blockIdx.y, group = a.group.d, splits = a.k_splits.d;
+  const auto [b, kv, pair] = pair_of(a.deal);
+  const int group = a.group.d, splits = a.k_splits.d;
   const int tile = splits > 1 ? a.k_splits.divide(blockIdx.z) : blockIdx.z, split = blockIdx.z - tile * splits;
   const auto [qs, ks] = spans_of(a.where, b);
   const int j0 = tile * KEYS;
@@ -380,7 +383,7 @@ hipError_t sequence_attention_backward(const SequenceAttention& x, void* workspa
   a.q = x.Q, a.k = x.K, a.v = x.V, a.o = x.O, a.go = x.dO, a.dq = x.dQ, a.dk = x.dK, a.dv = x.dV, a.lse = x.lse;
   a.q_stride = x.q_stride, a.k_stride = x.k_stride, a.v_stride = x.v_stride;
   a.dq_stride = x.dq_stride, a.dk_stride = x.dk_stride, a.dv_stride = x.dv_stride;
-  a.where = Packing(x);
+  a.where = Packing(x), a.deal = Deal(x, std::max(p.q_splits, p.k_splits));
   char* at = static_cast<char*>(workspace);
   a.lse2 = reinterpret_cast<float*>(at), at += p.stats;
   a.delta = reinterpret_cast<float*>(at), at += p.stats;
