@@ -143,45 +143,61 @@ __global__ __launch_bounds__(256) void catalogue_lse_kernel(Args a) {
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk) negate(x[kk]);
   }
+  // Two blocks of 32 items a step.  Each block's products are issued among the exponentials of the block before, which the matrix and the
+  // vector units then work on together.
   float m = -INFINITY, l = 0.f;
-  for (int i = 0; i < steps; ++i) {
+  auto absorb = [&](const f32x16& s) {
+    float top = s[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
+    const float to = fmaxf(m, pair_max(top) * c), base = to == -INFINITY ? 0.f : to;
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f(fmaf(s[e], c, -base));
+    l = fmaf(l, __builtin_amdgcn_exp2f(m - base), sum), m = to;
+  };
+  auto logits = [&](unsigned wt, int vb) {
+    f32x16 s = zero_block();
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) s = mma16(read.row(wt, 32 * vb, kk), x[kk], s);
+    return s;
+  };
+  f32x16 before;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) before[e] = -INFINITY;
+  auto arrived = [&](int i) -> unsigned {  // step i's tile; the next is asked for (past the last: nothing but zeros)
     wait_lds_loads<0>();
     lds_barrier();
-    if (i + 1 < steps) wl.issue(wm, (i + 1) * STEP, v1 - v0, smem + (i + 1) % 2 * Shape::kBytes, tid);
-    const unsigned wt = lds_offset_of(smem + i % 2 * Shape::kBytes);
-    f32x16 s[VB];
+    wl.issue(wm, (i + 1) * STEP, v1 - v0, smem + (i + 1) % 2 * Shape::kBytes, tid);
+    return lds_offset_of(smem + i % 2 * Shape::kBytes);
+  };
+  const int whole = (v1 - v0) / STEP;
+  for (int i = 0; i < whole; ++i) {
+    const unsigned wt = arrived(i);
 #pragma unroll
     for (int vb = 0; vb < VB; ++vb) {
-      s[vb] = zero_block();
+      const f32x16 s = logits(wt, vb);
+      absorb(before);
+      before = s;
+      if constexpr (sizeof(T) == 2) {
 #pragma unroll
-      for (int kk = 0; kk < NK; ++kk) s[vb] = mma16(read.row(wt, 32 * vb, kk), x[kk], s[vb]);
+        for (int e = 0; e < 16; ++e) __builtin_amdgcn_sched_group_barrier(0x008, 1, 0), __builtin_amdgcn_sched_group_barrier(0x100, 1, 0), __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+      }
     }
-    if (v0 + (i + 1) * STEP > v1) {
-      seldom();
-#pragma unroll
-      for (int vb = 0; vb < VB; ++vb)
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (v0 + i * STEP + 32 * vb + block_row(e, g) >= v1) s[vb][e] = -INFINITY;
-    }
-    float top = s[0][0];
-#pragma unroll
-    for (int vb = 0; vb < VB; ++vb)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[vb][e]);
-    top = pair_max(top) * c;
-    if (__any(top > m + kHeadroom)) {
-      seldom();
-      const float to = fmaxf(m, top);
-      l *= to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
-      m = to;
-    }
-    const float base = m == -INFINITY ? 0.f : m;
-#pragma unroll
-    for (int vb = 0; vb < VB; ++vb)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) l += __builtin_amdgcn_exp2f(fmaf(s[vb][e], c, -base));
   }
+  if (whole < steps) {
+    const unsigned wt = arrived(whole);
+#pragma unroll 1
+    for (int vb = 0; vb < VB; ++vb) {
+      absorb(before);
+      before = logits(wt + 32 * vb * Shape::kRowBytes, 0);
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (v0 + whole * STEP + 32 * vb + block_row(e, g) >= v1) before[e] = -INFINITY;
+    }
+  }
+  wait_lds_loads<0>();
+  absorb(before);
   l = pair_sum(l);
   if (row < count && g == 0) {
     float* to = a.parts + (static_cast<int64_t>(split) * a.rows + row) * 2;
