@@ -1,8 +1,8 @@
 // Softmax cross entropy of rows over a catalogue of items, with its gradients, the logits never in memory:
 //   z_iv = scale <X_i, W_v>,   lse_i = log sum_v exp(z_iv),   loss_i = lse_i - z_i,target(i)
 //   e_iv = dloss_i scale (exp(z_iv - lse_i) - [v = target(i)]),   dX_i = sum_v e_iv W_v,   dW_v = sum_i e_iv X_i.
-// Rows without a target have no loss and no gradients, and nothing of them is read into any: the other rows are listed first and,
-// where there are any to leave out, copied together (gather), so that padding costs no products.
+// Rows without a target have no loss and no gradients, and nothing of them is read into any: the other rows are listed first and, where
+// they are streamed and there are any to leave out, copied together (gather), so that padding costs no products.
 // The forward pass and dX hold rows of X in registers and stream the items' tiles, with the catalogue cut into chunks whose sums
 // are folded in ascending order; dW holds items and streams rows.  The target's own term of dX is added in fp32 at the fold.
 #include <algorithm>
@@ -30,8 +30,10 @@ struct Args {
   void* packed;       // [rows][d] the rows with a target, written where some have none
   float *c_lse2, *c_g, *c_e;  // [rows] of the listed rows: lse log2 e; dloss scale; e of the target
   int32_t* c_target;  // [rows]
-  float* parts;       // forward [splits][rows][2], dX [splits][rows][padded d], dW [splits][items][padded d]
-  int splits, chunk;
+  float* parts;       // forward [splits][rows][2], dX [splits][rows][padded d]
+  float* item_parts;  // dW [item_splits][items][padded d]
+  int splits, chunk;            // of the catalogue, for the kernels that hold rows
+  int item_splits, item_chunk;  // of the rows, for those that hold items
 };
 
 constexpr int kGatherRows = 64;  // rows a workgroup of the gather takes at a time
@@ -72,25 +74,23 @@ __global__ __launch_bounds__(256) void gather_kernel(Args a, int64_t each) {
         if constexpr (!BACKWARD) a.loss[i] = 0.f, a.lse[i] = 0.f;
       }
     }
-    if (whole && !BACKWARD) continue;
+    if constexpr (!BACKWARD) continue;
     __syncthreads();
     const int here = static_cast<int>(min<int64_t>(kGatherRows, end - at));
 #pragma unroll 4
     for (int r = wave; r < here; r += 4) {  // a wave a row
       const T* from = static_cast<const T*>(a.x) + (at + r) * a.d;
       const int to = place[r];
-      if constexpr (BACKWARD) {
-        if (to >= 0) {  // e of the row's own target, dloss scale (p - 1)
-          const T* w = static_cast<const T*>(a.w) + static_cast<int64_t>(a.targets[at + r]) * a.d;
-          float z = 0.f;
-          for (int c = lane; c < a.d; c += 64) z = fmaf(to_float(from[c]), to_float(w[c]), z);
-          z = wave_sum(z) * a.scale - a.lse[at + r];
-          if (lane == 0) a.c_e[to] = (__builtin_amdgcn_exp2f(z * kLog2e) - 1.f) * a.dloss[at + r] * a.scale;
-        }
-        if (whole) continue;
+      if (to >= 0) {  // e of the row's own target, dloss scale (p - 1)
+        const T* w = static_cast<const T*>(a.w) + static_cast<int64_t>(a.targets[at + r]) * a.d;
+        float z = 0.f;
+        for (int c = lane; c < a.d; c += 64) z = fmaf(to_float(from[c]), to_float(w[c]), z);
+        z = wave_sum(z) * a.scale - a.lse[at + r];
+        if (lane == 0) a.c_e[to] = (__builtin_amdgcn_exp2f(z * kLog2e) - 1.f) * a.dloss[at + r] * a.scale;
       }
+      if (whole) continue;
       T* dst = to >= 0 ? static_cast<T*>(a.packed) + static_cast<int64_t>(to) * a.d : static_cast<T*>(a.dx) + (at + r) * a.d;
-      if (to < 0 && (!BACKWARD || a.dx == nullptr)) continue;
+      if (to < 0 && a.dx == nullptr) continue;
       if (a.x_pieces && a.quads) {  // rows of whole 16-byte pieces: at most 64 of them
         const int c = lane * static_cast<int>(16 / sizeof(T));
         if (c < a.d) {
@@ -110,14 +110,26 @@ __global__ __launch_bounds__(256) void gather_kernel(Args a, int64_t each) {
   }
 }
 
-// The listed rows of X: X itself where every row is listed.
-template <typename T>
-__device__ __forceinline__ const T* listed_rows(const Args& a, int count) {
-  return static_cast<const T*>(count == a.rows ? a.x : a.packed);
+// Few rows are listed by every wave of the forward pass for itself: a look at all targets, 64 at a time, takes less than another
+// kernel.  The wave's 32 places from `first` on get the rows that stand there; returns how many rows are listed in all.
+constexpr int kFewRows = 4096;
+__device__ __forceinline__ int list_rows(const Args& a, int first, int lane, int32_t* places, bool zero_others) {
+  int before = 0;
+#pragma unroll 4
+  for (int base = 0; base < a.rows; base += 64) {
+    const int i = base + lane;
+    const bool x = i < a.rows && static_cast<unsigned>(a.targets[i]) < static_cast<unsigned>(a.items);
+    const unsigned long long votes = __ballot(x);
+    const int to = before + __popcll(votes & ((1ull << lane) - 1)) - first;
+    if (x && static_cast<unsigned>(to) < 32u) places[to] = i;
+    if (zero_others && !x && i < a.rows) a.loss[i] = 0.f, a.lse[i] = 0.f;
+    before += __popcll(votes);
+  }
+  wave_lds_fence();
+  return before;
 }
 
-// Running maximum and sum of a chunk of the catalogue for 32 rows a wave (as in the attention's forward pass, see there).
-constexpr float kHeadroom = 8.f;
+// Running maximum and sum of a chunk of the catalogue for 32 rows a wave.
 template <typename T, int D, int STEP>
 __global__ __launch_bounds__(256) void catalogue_lse_kernel(Args a) {
   using Shape = Tile<T, D, STEP>;
@@ -127,17 +139,30 @@ __global__ __launch_bounds__(256) void catalogue_lse_kernel(Args a) {
   extern __shared__ __align__(1024) unsigned char smem[];  // [2] tiles
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);
-  const int split = blockIdx.x % a.splits, tile = blockIdx.x / a.splits, count = a.live[0];
-  if (tile * 128 >= count) return;
-  const int row = tile * 128 + 32 * wave + n;
+  const int split = blockIdx.x % a.splits, tile = blockIdx.x / a.splits, row = tile * 128 + 32 * wave + n;
   const int v0 = split * a.chunk, v1 = min(a.items, v0 + a.chunk), steps = (v1 - v0 + STEP - 1) / STEP;
   const unsigned width = a.d * sizeof(T);
   const Rows wm{static_cast<const T*>(a.w) + static_cast<int64_t>(v0) * a.d, width, width, a.w_pieces};
   Loader wl;
   wl.init(wm, tid);
   wl.issue(wm, 0, v1 - v0, smem, tid);
+  int count, from = 0;
+  if (a.rows <= kFewRows) {
+    int32_t* places = reinterpret_cast<int32_t*>(smem + Shape::kBytes) + 32 * wave;  // (where the second tile will be)
+    count = list_rows(a, row - n, lane, places, split == 0 && tile == 0 && wave == 0);
+    if (row < count) from = places[n];
+    if (split == 0 && g == 0 && row < count) a.live[1 + row] = from;
+    if (split == 0 && row == 0 && g == 0) a.live[0] = count;
+  } else {
+    count = a.live[0];
+    if (row < count) from = a.live[1 + row];
+  }
+  if (tile * 128 >= count) {
+    wait_lds_loads<0>();
+    return;
+  }
   Fragment<T> x[NK];
-  load_row<T, D>(listed_rows<T>(a, count) + static_cast<int64_t>(row) * a.d, width, a.x_pieces, row < count, g, x);
+  load_row<T, D>(static_cast<const T*>(a.x) + static_cast<int64_t>(from) * a.d, width, a.x_pieces, row < count, g, x);
   const float c = fmaxf(fabsf(a.scale) * kLog2e, 1e-37f);
   if (a.scale < 0.f) {
 #pragma unroll
@@ -234,15 +259,14 @@ __global__ __launch_bounds__(256) void catalogue_loss_kernel(Args a) {
 
 // sum_v p_iv W_v over a chunk of the catalogue, 32 rows a wave.
 template <typename T, int D, int STEP>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void catalogue_dx_kernel(Args a) {
+__device__ __forceinline__ void rows_gradient(Args a, unsigned block, unsigned char* smem) {
   using Shape = Tile<T, D, STEP>;
   using Loader = TileLoader<T, D, STEP, 4>;
   using Reader = TileReader<T, D, STEP>;
   constexpr int VB = STEP / 32, NK = D / 16, OB = D / 32;
-  extern __shared__ __align__(1024) unsigned char smem[];  // [2] tiles
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);
-  const int split = blockIdx.x % a.splits, tile = blockIdx.x / a.splits, count = a.live[0];
+  const int split = block % a.splits, tile = block / a.splits, count = a.live[0];
   if (tile * 128 >= count) return;
   const int row = tile * 128 + 32 * wave + n;
   const int v0 = split * a.chunk, v1 = min(a.items, v0 + a.chunk), steps = (v1 - v0 + STEP - 1) / STEP;
@@ -252,7 +276,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void catalogue_dx_kern
   wl.init(wm, tid);
   wl.issue(wm, 0, v1 - v0, smem, tid);
   Fragment<T> x[NK];
-  load_row<T, D>(listed_rows<T>(a, count) + static_cast<int64_t>(row) * a.d, width, a.x_pieces, row < count, g, x);
+  load_row<T, D>(static_cast<const T*>(a.x) + static_cast<int64_t>(row < count ? a.live[1 + row] : 0) * a.d, width, a.x_pieces, row < count, g, x);
   const float c = a.scale * kLog2e, lse2 = row < count ? a.c_lse2[row] : 0.f;
   f32x16 dx[OB];
 #pragma unroll
@@ -291,9 +315,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void catalogue_dx_kern
 
 // dX_i = dloss_i scale (the chunks' sums - W_target).
 template <typename T, int D>
-__global__ __launch_bounds__(256) void catalogue_dx_fold_kernel(Args a, int groups) {
+__device__ __forceinline__ void fold_rows(const Args& a, unsigned block, int groups) {
   const Folder<D> at(groups);
-  const int row = blockIdx.x * at.rows + at.row, c = 4 * at.t;
+  const int row = block * at.rows + at.row, c = 4 * at.t;
   const bool live = row < a.live[0];
   f32x4 sum = at.sum(a.parts + static_cast<int64_t>(row) * D, a.rows * D, a.splits, groups, live);
   if (!live || at.group != 0) return;
@@ -307,19 +331,18 @@ __global__ __launch_bounds__(256) void catalogue_dx_fold_kernel(Args a, int grou
 
 // sum_i e_iv X_i over a chunk of the listed rows, 32 items a wave.
 template <typename T, int D, int STEP>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void catalogue_dw_kernel(Args a) {
+__device__ __forceinline__ void items_gradient(Args a, unsigned block, unsigned char* smem) {
   using Shape = Tile<T, D, STEP>;
   using Loader = TileLoader<T, D, STEP, 4>;
   using Reader = TileReader<T, D, STEP>;
   constexpr int RB = STEP / 32, NK = D / 16, OB = D / 32, kStage = Shape::kBytes + 1024;  // rows; lse2, dloss scale, target, its e, each [64]
-  extern __shared__ __align__(1024) unsigned char smem[];                                 // [2] stages
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);
-  const int split = blockIdx.x % a.splits, tile = blockIdx.x / a.splits, count = a.live[0];
+  const int split = block % a.item_splits, tile = block / a.item_splits, count = a.live[0];
   const int item0 = tile * 128 + 32 * wave, item = item0 + n;
-  const int i0 = split * a.chunk, i1 = min(count, i0 + a.chunk), steps = i1 > i0 ? (i1 - i0 + STEP - 1) / STEP : 0;
+  const int i0 = split * a.item_chunk, i1 = min(count, i0 + a.item_chunk), steps = i1 > i0 ? (i1 - i0 + STEP - 1) / STEP : 0;
   const unsigned width = a.d * sizeof(T);
-  const Rows xm{listed_rows<T>(a, count) + static_cast<int64_t>(i0) * a.d, width, width, a.x_pieces};
+  const Rows xm{static_cast<const T*>(count == a.rows ? a.x : a.packed) + static_cast<int64_t>(i0) * a.d, width, width, a.x_pieces};
   Loader xl;
   xl.init(xm, tid);
   auto ask = [&](int i) {
@@ -347,11 +370,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void catalogue_dw_kern
     const float* own = weight + 128;
     // which of the step's rows have one of the wave's items for their target (rows past the last: with the weight 0)
     const unsigned long long chosen = __ballot(lane < STEP && static_cast<unsigned>(target[lane % STEP] - item0) < 32u);
-#pragma unroll
+#pragma unroll(D < 256 ? RB : 1)
     for (int rb = 0; rb < RB; ++rb) {
+      const unsigned block = xt + 32 * rb * Shape::kRowBytes;
       f32x16 e = zero_block();
 #pragma unroll
-      for (int kk = 0; kk < NK; ++kk) e = mma16(read.row(xt, 32 * rb, kk), w[kk], e);
+      for (int kk = 0; kk < NK; ++kk) e = mma16(read.row(block, 0, kk), w[kk], e);
       auto weigh = [&](auto with_targets) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -373,7 +397,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void catalogue_dw_kern
       for (int f = 0; f < 2; ++f) {
         const Fragment<T> ef = half_fragment<T>(e, f);
 #pragma unroll
-        for (int ob = 0; ob < OB; ++ob) dw[ob] = mma16(read.column(xt, 32 * rb + 16 * f, 32 * ob), ef, dw[ob]);
+        for (int ob = 0; ob < OB; ++ob) dw[ob] = mma16(read.column(block, 16 * f, 32 * ob), ef, dw[ob]);
       }
     }
     // A target's e is near its row's whole weight and, in a large catalogue, rarely has company in its sum: what rounding took of it is
@@ -398,8 +422,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void catalogue_dw_kern
     }
   }
   if (item >= a.items) return;
-  if (a.splits > 1) {
-    float* to = a.parts + (static_cast<int64_t>(split) * a.items + item) * D;
+  if (a.item_splits > 1) {
+    float* to = a.item_parts + (static_cast<int64_t>(split) * a.items + item) * D;
 #pragma unroll
     for (int ob = 0; ob < OB; ++ob) store_block(to, dw[ob], 1.f, 32 * ob, D, true, g);
   } else {
@@ -410,12 +434,29 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void catalogue_dw_kern
 }
 
 template <typename T, int D>
-__global__ __launch_bounds__(256) void catalogue_dw_fold_kernel(Args a, int groups) {
+__device__ __forceinline__ void fold_items(const Args& a, unsigned block, int groups) {
   const Folder<D> at(groups);
-  const int64_t item = static_cast<int64_t>(blockIdx.x) * at.rows + at.row;
+  const int64_t item = static_cast<int64_t>(block) * at.rows + at.row;
   const bool live = item < a.items;
-  const f32x4 sum = at.sum(a.parts + item * D, static_cast<int64_t>(a.items) * D, a.splits, groups, live);
+  const f32x4 sum = at.sum(a.item_parts + item * D, static_cast<int64_t>(a.items) * D, a.item_splits, groups, live);
   if (live && at.group == 0) store_four(static_cast<T*>(a.dw) + item * a.d, sum, 4 * at.t, a.d, a.quads);
+}
+
+// Both gradients in one launch (neither needs the other): `item_blocks` workgroups hold items, the others rows.  At the largest width,
+// where either's operands fill the registers, a launch each.
+constexpr int kItems = 1, kRowsOf = 2;
+template <typename T, int D, int STEP, int SIDES>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void catalogue_gradients_kernel(Args a, unsigned item_blocks) {
+  extern __shared__ __align__(1024) unsigned char smem[];  // [2] stages
+  if constexpr (SIDES == kItems) items_gradient<T, D, STEP>(a, blockIdx.x, smem);
+  else if constexpr (SIDES == kRowsOf) rows_gradient<T, D, STEP>(a, blockIdx.x, smem);
+  else if (blockIdx.x < item_blocks) items_gradient<T, D, STEP>(a, blockIdx.x, smem);
+  else rows_gradient<T, D, STEP>(a, blockIdx.x - item_blocks, smem);
+}
+template <typename T, int D>
+__global__ __launch_bounds__(256) void catalogue_fold_kernel(Args a, unsigned item_blocks, int item_groups, int row_groups) {
+  if (blockIdx.x < item_blocks) fold_items<T, D>(a, blockIdx.x, item_groups);
+  else fold_rows<T, D>(a, blockIdx.x - item_blocks, row_groups);
 }
 
 int padded(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
@@ -434,7 +475,7 @@ Cut cut(int64_t tiles, int64_t length, int step, int64_t want) {
 
 struct Plan {
   Cut rows, items;  // of the kernels that hold rows (chunks of items), that hold items (chunks of rows)
-  size_t live, packed, listed, parts, bytes;
+  size_t live, packed, listed, parts, item_parts, bytes;
 };
 Plan plan_of(int64_t rows, int items, int d, int dtype, bool backward) {
   Plan p{};
@@ -443,12 +484,11 @@ Plan plan_of(int64_t rows, int items, int d, int dtype, bool backward) {
   p.rows = cut((rows + 127) / 128, items, step, want);
   p.items = cut((static_cast<int64_t>(items) + 127) / 128, rows, step, want);
   p.live = align_up((rows + 1) * sizeof(int32_t));
-  p.packed = align_up(static_cast<size_t>(rows) * d * (dtype == 1 ? 2 : 4));
+  p.packed = backward ? align_up(static_cast<size_t>(rows) * d * (dtype == 1 ? 2 : 4)) : 0;
   p.listed = backward ? align_up(rows * sizeof(float)) : 0;
-  const size_t by_rows = static_cast<size_t>(p.rows.splits) * rows * (backward ? D : 2) * sizeof(float);
-  const size_t by_items = backward && p.items.splits > 1 ? static_cast<size_t>(p.items.splits) * items * D * sizeof(float) : 0;
-  p.parts = align_up(std::max(by_rows, by_items));
-  p.bytes = p.live + p.packed + 4 * p.listed + p.parts;
+  p.parts = align_up(static_cast<size_t>(p.rows.splits) * rows * (backward ? D : 2) * sizeof(float));
+  p.item_parts = backward && p.items.splits > 1 ? align_up(static_cast<size_t>(p.items.splits) * items * D * sizeof(float)) : 0;
+  p.bytes = p.live + p.packed + 4 * p.listed + p.parts + p.item_parts;
   return p;
 }
 
@@ -468,7 +508,9 @@ Args args_of(const CatalogueLoss& x, const Plan& p, void* workspace) {
   a.c_g = reinterpret_cast<float*>(at), at += p.listed;
   a.c_e = reinterpret_cast<float*>(at), at += p.listed;
   a.c_target = reinterpret_cast<int32_t*>(at), at += p.listed;
-  a.parts = reinterpret_cast<float*>(at);
+  a.parts = reinterpret_cast<float*>(at), at += p.parts;
+  a.item_parts = reinterpret_cast<float*>(at);
+  a.splits = p.rows.splits, a.chunk = p.rows.chunk, a.item_splits = p.items.splits, a.item_chunk = p.items.chunk;
   return a;
 }
 
@@ -479,55 +521,56 @@ hipError_t gather(const Args& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <typename K>
-hipError_t launch(PerDevice& granted, K kernel, int64_t blocks, int lds, const Args& a, hipStream_t s) {
+template <typename K, typename... A>
+hipError_t launch(PerDevice& granted, K kernel, int64_t blocks, int lds, hipStream_t s, A... args) {
   if (hipError_t e = allow_lds(granted, reinterpret_cast<const void*>(kernel), lds); e != hipSuccess) return e;
-  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), lds, s, a);
+  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), lds, s, args...);
   return hipGetLastError();
 }
 
 template <typename T, int D>
-hipError_t forward(Args a, const Plan& p, hipStream_t s) {
+hipError_t forward(const Args& a, hipStream_t s) {
   constexpr int STEP = sizeof(T) == 2 ? 64 : 32;
-  if (hipError_t e = gather<T, false>(a, s); e != hipSuccess) return e;
+  if (a.rows > kFewRows)
+    if (hipError_t e = gather<T, false>(a, s); e != hipSuccess) return e;
   static PerDevice granted;
-  a.splits = p.rows.splits, a.chunk = p.rows.chunk;
-  if (hipError_t e = launch(granted, catalogue_lse_kernel<T, D, STEP>, (a.rows + 127) / 128 * a.splits, 2 * Tile<T, D, STEP>::kBytes, a, s); e != hipSuccess) return e;
+  if (hipError_t e = launch(granted, catalogue_lse_kernel<T, D, STEP>, (a.rows + 127) / 128 * a.splits, 2 * Tile<T, D, STEP>::kBytes, s, a); e != hipSuccess) return e;
   hipLaunchKernelGGL(catalogue_loss_kernel<T>, dim3(static_cast<unsigned>((a.rows + 3) / 4)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
 template <typename T, int D>
-hipError_t backward(Args a, const Plan& p, hipStream_t s) {
+hipError_t backward(const Args& a, hipStream_t s) {
   constexpr int STEP = sizeof(T) == 2 ? 64 : 32;
   if (hipError_t e = gather<T, true>(a, s); e != hipSuccess) return e;
-  if (a.dx) {
+  const int64_t item_blocks = a.dw ? (static_cast<int64_t>(a.items) + 127) / 128 * a.item_splits : 0, row_blocks = a.dx ? (a.rows + 127) / 128 * a.splits : 0;
+  constexpr int lds = 2 * (Tile<T, D, STEP>::kBytes + 1024);
+  if constexpr (D < kMaxCatalogueWidth) {
     static PerDevice granted;
-    a.splits = p.rows.splits, a.chunk = p.rows.chunk;
-    if (hipError_t e = launch(granted, catalogue_dx_kernel<T, D, STEP>, (a.rows + 127) / 128 * a.splits, 2 * Tile<T, D, STEP>::kBytes, a, s); e != hipSuccess) return e;
-    const int groups = fold_groups(a.splits, D / 4), per = 256 / (D / 4) / groups;
-    hipLaunchKernelGGL((catalogue_dx_fold_kernel<T, D>), dim3(static_cast<unsigned>((a.rows + per - 1) / per)), dim3(256), 0, s, a, groups);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    if (hipError_t e = launch(granted, catalogue_gradients_kernel<T, D, STEP, kItems + kRowsOf>, item_blocks + row_blocks, lds, s, a, static_cast<unsigned>(item_blocks));
+        e != hipSuccess)
+      return e;
+  } else {
+    static PerDevice items_granted, rows_granted;
+    if (item_blocks > 0)
+      if (hipError_t e = launch(items_granted, catalogue_gradients_kernel<T, D, STEP, kItems>, item_blocks, lds, s, a, 0u); e != hipSuccess) return e;
+    if (row_blocks > 0)
+      if (hipError_t e = launch(rows_granted, catalogue_gradients_kernel<T, D, STEP, kRowsOf>, row_blocks, lds, s, a, 0u); e != hipSuccess) return e;
   }
-  if (a.dw) {
-    static PerDevice granted;
-    a.splits = p.items.splits, a.chunk = p.items.chunk;
-    const int64_t tiles = (static_cast<int64_t>(a.items) + 127) / 128;
-    if (hipError_t e = launch(granted, catalogue_dw_kernel<T, D, STEP>, tiles * a.splits, 2 * (Tile<T, D, STEP>::kBytes + 1024), a, s); e != hipSuccess) return e;
-    if (a.splits > 1) {
-      const int groups = fold_groups(a.splits, D / 4), per = 256 / (D / 4) / groups;
-      hipLaunchKernelGGL((catalogue_dw_fold_kernel<T, D>), dim3(static_cast<unsigned>((static_cast<int64_t>(a.items) + per - 1) / per)), dim3(256), 0, s, a, groups);
-      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    }
-  }
-  return hipSuccess;
+  const int item_groups = fold_groups(a.item_splits, D / 4), row_groups = fold_groups(a.splits, D / 4);
+  auto folds = [](int64_t rows, int groups) { const int64_t per = 256 / (D / 4) / groups; return (rows + per - 1) / per; };
+  const int64_t item_folds = a.dw && a.item_splits > 1 ? folds(a.items, item_groups) : 0, row_folds = a.dx ? folds(a.rows, row_groups) : 0;
+  if (item_folds + row_folds == 0) return hipSuccess;
+  hipLaunchKernelGGL((catalogue_fold_kernel<T, D>), dim3(static_cast<unsigned>(item_folds + row_folds)), dim3(256), 0, s, a, static_cast<unsigned>(item_folds), item_groups,
+                     row_groups);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 bool catalogue_loss_fits(int64_t rows, int items) {  // 2^32 work items a launch
   const int64_t tiles = std::max((rows + 127) / 128, (static_cast<int64_t>(items) + 127) / 128);
-  return rows < (int64_t{1} << 26) - 128 && items <= (1 << 30) && (tiles + 2 * compute_units()) * 256 < (int64_t{1} << 32);
+  return rows < (int64_t{1} << 25) && items <= (1 << 30) && (tiles + 4 * compute_units()) * 256 < (int64_t{1} << 32);
 }
 
 size_t catalogue_loss_workspace(int64_t rows, int items, int d, int dtype, bool backward) { return plan_of(rows, items, d, dtype, backward).bytes; }
@@ -536,16 +579,16 @@ hipError_t catalogue_loss(const CatalogueLoss& x, void* workspace, hipStream_t s
   const Plan p = plan_of(x.rows, x.items, x.d, x.dtype, false);
   const Args a = args_of(x, p, workspace);
   const int D = padded(x.d);
-  if (x.dtype == 1) return D == 64 ? forward<bf16_t, 64>(a, p, s) : D == 128 ? forward<bf16_t, 128>(a, p, s) : forward<bf16_t, 256>(a, p, s);
-  return D == 64 ? forward<float, 64>(a, p, s) : D == 128 ? forward<float, 128>(a, p, s) : forward<float, 256>(a, p, s);
+  if (x.dtype == 1) return D == 64 ? forward<bf16_t, 64>(a, s) : D == 128 ? forward<bf16_t, 128>(a, s) : forward<bf16_t, 256>(a, s);
+  return D == 64 ? forward<float, 64>(a, s) : D == 128 ? forward<float, 128>(a, s) : forward<float, 256>(a, s);
 }
 
 hipError_t catalogue_loss_backward(const CatalogueLoss& x, void* workspace, hipStream_t s) {
   const Plan p = plan_of(x.rows, x.items, x.d, x.dtype, true);
   const Args a = args_of(x, p, workspace);
   const int D = padded(x.d);
-  if (x.dtype == 1) return D == 64 ? backward<bf16_t, 64>(a, p, s) : D == 128 ? backward<bf16_t, 128>(a, p, s) : backward<bf16_t, 256>(a, p, s);
-  return D == 64 ? backward<float, 64>(a, p, s) : D == 128 ? backward<float, 128>(a, p, s) : backward<float, 256>(a, p, s);
+  if (x.dtype == 1) return D == 64 ? backward<bf16_t, 64>(a, s) : D == 128 ? backward<bf16_t, 128>(a, s) : backward<bf16_t, 256>(a, s);
+  return D == 64 ? backward<float, 64>(a, s) : D == 128 ? backward<float, 128>(a, s) : backward<float, 256>(a, s);
 }
 
 }  // namespace lime
