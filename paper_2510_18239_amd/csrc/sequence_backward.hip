@@ -279,12 +279,12 @@ __global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
   }
 }
 
-// The chunks' sums of a row of dQ (what = 0), dK (1) or dV (2) folded.
+// The chunks' sums folded: of dQ where its keys were cut (q_heads = hq, otherwise 0), then of dK and dV where the queries were.
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void sequence_attention_fold_kernel(Args a, int what, int groups) {
+__global__ __launch_bounds__(256) void sequence_attention_fold_kernel(Args a, int q_heads, int groups) {
   const Folder<DH> at(groups);
-  const int heads = what == 0 ? a.hq : a.hk, splits = what == 0 ? a.q_splits.d : a.k_splits.d;
-  const int b = blockIdx.y, head = blockIdx.x, i = blockIdx.z * at.rows + at.row;
+  const int h = blockIdx.x - q_heads, what = h < 0 ? 0 : h < a.hk ? 1 : 2, head = h < 0 ? blockIdx.x : h - (what - 1) * a.hk;
+  const int b = blockIdx.y, i = blockIdx.z * at.rows + at.row, heads = what == 0 ? a.hq : a.hk, splits = what == 0 ? a.q_splits.d : a.k_splits.d;
   const Spans spans = spans_of(a.where, b);
   const Span span = what == 0 ? spans.q : spans.k;
   const bool live = i < span.slot;
@@ -328,13 +328,6 @@ Plan plan_of(const SequenceAttention& a) {
 }
 
 template <typename T, int DH>
-hipError_t fold(const Args& a, int what, int users, int most, int heads, int splits, hipStream_t s) {
-  const int groups = fold_groups(splits, DH / 4), per = 256 / (DH / 4) / groups;
-  hipLaunchKernelGGL((sequence_attention_fold_kernel<T, DH>), dim3(heads, users, (most + per - 1) / per), dim3(256), 0, s, a, what, groups);
-  return hipGetLastError();
-}
-
-template <typename T, int DH>
 hipError_t run(Args a, const Plan& p, int users, hipStream_t s) {
   constexpr int STEP = sizeof(T) == 2 ? 64 : 32;
   const int max_q = a.where.max_q, max_k = a.where.max_k;
@@ -346,18 +339,21 @@ hipError_t run(Args a, const Plan& p, int users, hipStream_t s) {
     a.tiles = p.q_tiles;
     hipLaunchKernelGGL(kernel, dim3(a.hk, users, p.q_tiles * p.q_splits), dim3(256), lds, s, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    if (p.q_splits > 1)
-      if (hipError_t e = fold<T, DH>(a, 0, users, max_q, a.hq, p.q_splits, s); e != hipSuccess) return e;
   }
-  if (max_k == 0) return hipSuccess;
-  constexpr int lds = 2 * (2 * Tile<T, DH, STEP>::kBytes + 512);
-  static PerDevice granted;
-  const auto kernel = sequence_attention_dkv_kernel<T, DH, STEP>;
-  if (hipError_t e = allow_lds(granted, reinterpret_cast<const void*>(kernel), lds); e != hipSuccess) return e;
-  hipLaunchKernelGGL(kernel, dim3(a.hk, users, p.k_tiles * p.k_splits), dim3(256), lds, s, a);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess || p.k_splits == 1) return e;
-  if (hipError_t e = fold<T, DH>(a, 1, users, max_k, a.hk, p.k_splits, s); e != hipSuccess) return e;
-  return fold<T, DH>(a, 2, users, max_k, a.hk, p.k_splits, s);
+  if (max_k > 0) {
+    constexpr int lds = 2 * (2 * Tile<T, DH, STEP>::kBytes + 512);
+    static PerDevice granted;
+    const auto kernel = sequence_attention_dkv_kernel<T, DH, STEP>;
+    if (hipError_t e = allow_lds(granted, reinterpret_cast<const void*>(kernel), lds); e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3(a.hk, users, p.k_tiles * p.k_splits), dim3(256), lds, s, a);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  const bool q_folds = p.q_splits > 1 && max_q > 0, k_folds = p.k_splits > 1 && max_k > 0;
+  if (!q_folds && !k_folds) return hipSuccess;
+  const int groups = fold_groups(std::max(q_folds ? p.q_splits : 1, k_folds ? p.k_splits : 1), DH / 4), per = 256 / (DH / 4) / groups;
+  const int q_heads = q_folds ? a.hq : 0, most = std::max(q_folds ? max_q : 0, k_folds ? max_k : 0);
+  hipLaunchKernelGGL((sequence_attention_fold_kernel<T, DH>), dim3(q_heads + (k_folds ? 2 * a.hk : 0), users, (most + per - 1) / per), dim3(256), 0, s, a, q_heads, groups);
+  return hipGetLastError();
 }
 
 bool multiple(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
@@ -369,9 +365,10 @@ bool sequence_attention_backward_fits(const SequenceAttention& a) {  // 2^32 wor
   if (rows >= (int64_t{1} << 31) - 128 || pairs >= (int64_t{1} << 24)) return false;
   const Plan p = plan_of(a);
   const int64_t q_deep = static_cast<int64_t>(p.q_tiles) * p.q_splits, k_deep = static_cast<int64_t>(p.k_tiles) * p.k_splits;
-  auto folds = [&](int most, int heads) { return most < 65536 && a.B * static_cast<int64_t>(most) * heads < (int64_t{1} << 24); };
+  auto folds = [&](int most, int heads) { return most < 65536 && a.B * static_cast<int64_t>(most) * heads < (int64_t{1} << 22); };
   return q_deep < 65536 && k_deep < 65536 && pairs * q_deep < (int64_t{1} << 24) && pairs * k_deep < (int64_t{1} << 24) &&
-         (p.q_splits == 1 || folds(a.max_q, a.hq)) && (p.k_splits == 1 || folds(a.max_k, a.hk));
+         (p.q_splits == 1 || folds(a.max_q, a.hq)) && (p.k_splits == 1 || folds(a.max_k, 2 * a.hk)) &&
+         (p.q_splits == 1 || p.k_splits == 1 || folds(std::max(a.max_q, a.max_k), a.hq + 2 * a.hk));
 }
 
 size_t sequence_attention_backward_workspace(const SequenceAttention& a) { return plan_of(a).bytes; }
