@@ -279,12 +279,14 @@ __global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
   }
 }
 
-// The chunks' sums folded: of dQ where its keys were cut (q_heads = hq, otherwise 0), then of dK and dV where the queries were.
+// The chunks' sums folded: of dQ by the first q_blocks workgroups of a user where its keys were cut, then of dK and dV where the queries were.
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void sequence_attention_fold_kernel(Args a, int q_heads, int groups) {
+__global__ __launch_bounds__(256) void sequence_attention_fold_kernel(Args a, unsigned q_blocks, int groups) {
   const Folder<DH> at(groups);
-  const int h = blockIdx.x - q_heads, what = h < 0 ? 0 : h < a.hk ? 1 : 2, head = h < 0 ? blockIdx.x : h - (what - 1) * a.hk;
-  const int b = blockIdx.y, i = blockIdx.z * at.rows + at.row, heads = what == 0 ? a.hq : a.hk, splits = what == 0 ? a.q_splits.d : a.k_splits.d;
+  const bool of_q = blockIdx.x < q_blocks;
+  const int block = of_q ? blockIdx.x : blockIdx.x - q_blocks, heads = of_q ? a.hq : a.hk, each = of_q ? heads : 2 * heads;
+  const int tile = block / each, h = block - tile * each, what = of_q ? 0 : h < heads ? 1 : 2, head = what == 2 ? h - heads : h;
+  const int b = blockIdx.y, i = tile * at.rows + at.row, splits = of_q ? a.q_splits.d : a.k_splits.d;
   const Spans spans = spans_of(a.where, b);
   const Span span = what == 0 ? spans.q : spans.k;
   const bool live = i < span.slot;
@@ -351,8 +353,9 @@ hipError_t run(Args a, const Plan& p, int users, hipStream_t s) {
   const bool q_folds = p.q_splits > 1 && max_q > 0, k_folds = p.k_splits > 1 && max_k > 0;
   if (!q_folds && !k_folds) return hipSuccess;
   const int groups = fold_groups(std::max(q_folds ? p.q_splits : 1, k_folds ? p.k_splits : 1), DH / 4), per = 256 / (DH / 4) / groups;
-  const int q_heads = q_folds ? a.hq : 0, most = std::max(q_folds ? max_q : 0, k_folds ? max_k : 0);
-  hipLaunchKernelGGL((sequence_attention_fold_kernel<T, DH>), dim3(q_heads + (k_folds ? 2 * a.hk : 0), users, (most + per - 1) / per), dim3(256), 0, s, a, q_heads, groups);
+  auto blocks = [&](int rows, int heads) { return static_cast<unsigned>((rows + per - 1) / per * heads); };
+  const unsigned q_blocks = q_folds ? blocks(max_q, a.hq) : 0, k_blocks = k_folds ? blocks(max_k, 2 * a.hk) : 0;
+  hipLaunchKernelGGL((sequence_attention_fold_kernel<T, DH>), dim3(q_blocks + k_blocks, users), dim3(256), 0, s, a, q_blocks, groups);
   return hipGetLastError();
 }
 
@@ -365,10 +368,8 @@ bool sequence_attention_backward_fits(const SequenceAttention& a) {  // 2^32 wor
   if (rows >= (int64_t{1} << 31) - 128 || pairs >= (int64_t{1} << 24)) return false;
   const Plan p = plan_of(a);
   const int64_t q_deep = static_cast<int64_t>(p.q_tiles) * p.q_splits, k_deep = static_cast<int64_t>(p.k_tiles) * p.k_splits;
-  auto folds = [&](int most, int heads) { return most < 65536 && a.B * static_cast<int64_t>(most) * heads < (int64_t{1} << 22); };
-  return q_deep < 65536 && k_deep < 65536 && pairs * q_deep < (int64_t{1} << 24) && pairs * k_deep < (int64_t{1} << 24) &&
-         (p.q_splits == 1 || folds(a.max_q, a.hq)) && (p.k_splits == 1 || folds(a.max_k, 2 * a.hk)) &&
-         (p.q_splits == 1 || p.k_splits == 1 || folds(std::max(a.max_q, a.max_k), a.hq + 2 * a.hk));
+  // (of a side that is cut, users times heads times rows are less than 2^17: a side with more has workgroups enough)
+  return q_deep < 65536 && k_deep < 65536 && pairs * q_deep < (int64_t{1} << 24) && pairs * k_deep < (int64_t{1} << 24);
 }
 
 size_t sequence_attention_backward_workspace(const SequenceAttention& a) { return plan_of(a).bytes; }

@@ -208,8 +208,7 @@ struct TileLoader {
       resource[3] = 0x00020000u;
       const unsigned lds = __builtin_amdgcn_readfirstlane(lds_offset_of(tile) + (tid >> 6) * 1024);
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i)
-{
+      for (int i = 0; i < kLoads; ++i) {
         unsigned at_row;  // (added here, not by the compiler: it would keep all the sums in registers across the kernel's loop)
         asm volatile("s_mov_b32 m0, %1\n\tv_add_u32_e32 %0, %2, %3\n\tbuffer_load_dwordx4 %0, %4, 0 offen lds"
                      : "=&v"(at_row)

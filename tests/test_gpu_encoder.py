@@ -183,6 +183,10 @@ def test_slots_and_lengths(dtype, q_lens, k_lens, slots, hq, hk, dh, causal):
     attention_case(dtype, q_lens, k_lens, hq, hk, dh, causal, slots)
 
 
+def test_many_heads_on_one_key_head():
+    attention_case("bf16", [1], [21000], 200, 1, 32)  # both sides of the backward pass are cut into chunks
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("before", [1, 8, 64])
 @pytest.mark.parametrize("dh", [64, 33])
