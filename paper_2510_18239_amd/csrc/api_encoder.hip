@@ -141,8 +141,8 @@ int32_t lime_norm_rotary_backward(const void* dQO, int64_t dqo_stride, const voi
 
 size_t lime_sequence_attention_workspace_bytes(const lime_sequences* where, int32_t hq, int32_t hk, int32_t dh, int32_t dtype, int32_t backward) {
   if (!where || !known(dtype) || where->B <= 0 || hq <= 0 || hk <= 0 || hq % hk != 0 || dh <= 0 || dh > lime::kMaxSequenceHead || where->q_rows < 0 || where->k_rows < 0 ||
-      where->max_q < 0 || where->max_k < 0)
-    return 0;
+      where->max_q < 0 || where->max_k < 0 || where->q_rows > kMostRows || where->k_rows > kMostRows || where->B > 65535 || hq > 65535)
+    return 0;  // (within these the plan's products stay in 64 bits)
   const lime::SequenceAttention a = describe(where, hq, hk, dh, 1.f, 1, dtype);
   return backward ? lime::sequence_attention_backward_workspace(a) : lime::sequence_attention_workspace(a);
 }

@@ -569,8 +569,7 @@ hipError_t backward(const Args& a, hipStream_t s) {
 }  // namespace
 
 bool catalogue_loss_fits(int64_t rows, int items) {  // 2^32 work items a launch
-  const int64_t tiles = std::max((rows + 127) / 128, (static_cast<int64_t>(items) + 127) / 128);
-  return rows < (int64_t{1} << 25) && items <= (1 << 30) && (tiles + 4 * compute_units()) * 256 < (int64_t{1} << 32);
+  return rows < (int64_t{1} << 25) && items <= (1 << 30);
 }
 
 size_t catalogue_loss_workspace(int64_t rows, int items, int d, int dtype, bool backward) { return plan_of(rows, items, d, dtype, backward).bytes; }

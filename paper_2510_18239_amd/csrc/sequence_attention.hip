@@ -267,7 +267,7 @@ bool sequence_attention_fits(const SequenceAttention& a) {  // 2^32 work items a
   if (rows >= (int64_t{1} << 31) - 128 || pairs >= (int64_t{1} << 24)) return false;
   const Plan p = plan_of(a);
   const int64_t deep = static_cast<int64_t>(p.tiles) * p.splits;
-  return deep < 65536 && pairs * deep < (int64_t{1} << 26) / p.waves && (p.splits == 1 || (rows < 65536 && pairs * rows < (int64_t{1} << 24)));
+  return deep < 65536 && pairs * deep < (int64_t{1} << 26) / p.waves;  // (where keys are cut, pairs times rows are less than 2^17)
 }
 
 size_t sequence_attention_workspace(const SequenceAttention& a) { return std::max<size_t>(plan_of(a).bytes, 256); }

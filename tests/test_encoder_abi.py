@@ -96,6 +96,11 @@ def test_attention_workspace():
     few = dict(B=4, max_q=1, q_rows=4, max_k=100000, k_rows=400000)
     assert ask(**few) > 4 * 64 * 4 * 4  # the chunks' states
     assert ask(q_rows=0, k_rows=0) >= 256
+    most = dict(B=1 << 30, q_rows=1 << 40, k_rows=1 << 40, max_q=(1 << 31) - 1, max_k=(1 << 31) - 1)
+    assert ask(0, 1 << 30, 1 << 30, **most) == 0 and ask(1, 1 << 30, 1 << 30, **most) == 0  # past the limits: their products pass 64 bits
+    largest = dict(B=65535, q_rows=(1 << 31) - 1, k_rows=(1 << 31) - 1, max_q=(1 << 31) - 1, max_k=(1 << 31) - 1)
+    assert ask(0, 65535, 65535, **largest) >= 256 and ask(1, 65535, 65535, **largest) > 0
+    assert binding.lib().lime_catalogue_loss_workspace_bytes((1 << 63) - 1, 10, 64, 1, 1) == 0
 
 
 def loss(X=FAKE, W=FAKE, t=FAKE, out=FAKE, lse=FAKE, rows=10, items=20, d=64, dtype=1, ws=FAKE, ws_bytes=0):
