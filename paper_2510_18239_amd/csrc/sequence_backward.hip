@@ -2,7 +2,7 @@
 //   p_ij = exp(scale <Q_i, K_j> - lse_i),  D_i = <G_i, O_i>,  e_ij = p_ij (<G_i, V_j> - D_i):
 //   dQ_i = scale sum_j e_ij K_j,   dK_j = scale sum_i e_ij Q_i,   dV_j = sum_i p_ij G_i   (i over all heads that share the key head).
 // Two kernels, each with one side's rows and sums in registers while the other side's tiles stream past, so that every sum has one
-// owner and one order (no atomics): the first holds queries (rows as in the forward pass) and also leaves D and lse, by head, for
+// owner and one order (no atomics): the first holds queries (rows as in the forward pass) and also leaves -D and lse, by head, for
 // the second, which holds keys.  Seven products of the tiles where a kernel that kept both sides' sums would do five: the sums of
 // the other side would have to meet in memory.  Where the workgroups of a side are too few for the chip, the side that streams past is
 // cut into chunks whose sums a third kernel folds (fold.hpp).  p and e are rounded to the storage type, as operands of the last products.
@@ -20,7 +20,7 @@ struct Args {
   Packing where;
   Deal deal;
   const float* lse;
-  float *lse2, *delta;  // [hq][q_rows]: lse log2 e, D
+  float *lse2, *less;  // [hq][q_rows]: lse log2 e, -D
   void *dq, *dk, *dv;
   float *part_q, *part_kv;  // chunks > 1: [q_splits][q_rows][hq][padded dh], [k_splits][2][k_rows][hk][padded dh]
   Divisor group, q_splits, k_splits;
@@ -105,11 +105,13 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
   }
   if (live && g == 0 && split == 0) {
     const int64_t at = head * static_cast<int64_t>(a.where.q_rows) + qs.start + query;
-    a.lse2[at] = lse2, a.delta[at] = delta;
+    a.lse2[at] = lse2, a.less[at] = -delta;
   }
-  f32x16 dq[OB];
+  f32x16 dq[OB], less;  // less: -D, where the sums <G_i, V_j> - D_i start from
 #pragma unroll
   for (int ob = 0; ob < OB; ++ob) dq[ob] = zero_block();
+#pragma unroll
+  for (int x = 0; x < 16; ++x) less[x] = -delta;
 
   for (int i = 0; i < steps; ++i) {
     wait_lds_loads<0>();
@@ -121,14 +123,14 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
     const bool partial = key0 + KEYS > wave_least;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
-      f32x16 s = zero_block(), e = zero_block();
+      f32x16 s = zero_block(), e = less;
 #pragma unroll
       for (int kk = 0; kk < NK; ++kk) {
         s = mma16(read.row(kt, 32 * kb, kk), q[kk], s);
         e = mma16(read.row(vt, 32 * kb, kk), go[kk], e);
       }
 #pragma unroll
-      for (int x = 0; x < 16; ++x) e[x] = __builtin_amdgcn_exp2f(fmaf(s[x], c, -lse2)) * (e[x] - delta);
+      for (int x = 0; x < 16; ++x) e[x] *= __builtin_amdgcn_exp2f(fmaf(s[x], c, -lse2));
       if (partial) {
         seldom();
 #pragma unroll
@@ -161,7 +163,7 @@ __global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
   using Loader = TileLoader<T, DH, STEP, 4>;
   using Reader = TileReader<T, DH, STEP>;
   constexpr int QB = STEP / 32, OB = DH / 32, NK = DH / 16, KEYS = 128;
-  constexpr int kStage = 2 * Shape::kBytes + 512;          // queries, output gradients, lse2 [64], delta [64]
+  constexpr int kStage = 2 * Shape::kBytes + 512;          // queries, output gradients, lse2 [64], -D [64]
   extern __shared__ __align__(1024) unsigned char smem[];  // [2] stages
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);
@@ -196,7 +198,7 @@ __global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
     ql.issue(qm, ask_at, qs.used - begin, to, tid);
     gl.issue(gm, ask_at, qs.used - begin, to + Shape::kBytes, tid);
     if (wave < 2) {
-      const float* from = (wave == 0 ? a.lse2 : a.delta) + (kv * group + ask_head) * static_cast<int64_t>(a.where.q_rows) + qs.start + begin + ask_at;
+      const float* from = (wave == 0 ? a.lse2 : a.less) + (kv * group + ask_head) * static_cast<int64_t>(a.where.q_rows) + qs.start + begin + ask_at;
       words_to_lds(from, min(count, STEP), reinterpret_cast<float*>(to + 2 * Shape::kBytes) + 64 * wave, lane);
     }
     ask_at += STEP;
@@ -224,11 +226,17 @@ __global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
     if (q0 + STEP <= wave_first) continue;
     const unsigned char* tiles = smem + i % 2 * kStage;
     const unsigned qt = lds_offset_of(tiles), gt = qt + Shape::kBytes;
-    const float *lse2 = reinterpret_cast<const float*>(tiles + 2 * Shape::kBytes), *delta = lse2 + 64;
+    const float *lse2 = reinterpret_cast<const float*>(tiles + 2 * Shape::kBytes), *less = lse2 + 64;
     const bool partial = q0 < wave_all || q0 + STEP > qs.used;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-      f32x16 p = zero_block(), e = zero_block();
+      f32x16 p = zero_block(), e;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f32x4 d4 = *reinterpret_cast<const f32x4*>(less + 32 * qb + 8 * j + 4 * g);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) e[4 * j + x] = d4[x];
+      }
 #pragma unroll
       for (int kk = 0; kk < NK; ++kk) {
         p = mma16(read.row(qt, 32 * qb, kk), k[kk], p);
@@ -236,11 +244,11 @@ __global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const f32x4 l4 = *reinterpret_cast<const f32x4*>(lse2 + 32 * qb + 8 * j + 4 * g), d4 = *reinterpret_cast<const f32x4*>(delta + 32 * qb + 8 * j + 4 * g);
+        const f32x4 l4 = *reinterpret_cast<const f32x4*>(lse2 + 32 * qb + 8 * j + 4 * g);
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           p[4 * j + x] = __builtin_amdgcn_exp2f(fmaf(p[4 * j + x], c, -l4[x]));
-          e[4 * j + x] = p[4 * j + x] * (e[4 * j + x] - d4[x]);
+          e[4 * j + x] *= p[4 * j + x];
         }
       }
       if (partial) {
@@ -384,7 +392,7 @@ hipError_t sequence_attention_backward(const SequenceAttention& x, void* workspa
   a.where = Packing(x), a.deal = Deal(x, std::max(p.q_splits, p.k_splits));
   char* at = static_cast<char*>(workspace);
   a.lse2 = reinterpret_cast<float*>(at), at += p.stats;
-  a.delta = reinterpret_cast<float*>(at), at += p.stats;
+  a.less = reinterpret_cast<float*>(at), at += p.stats;
   a.part_q = reinterpret_cast<float*>(at), at += p.part_q;
   a.part_kv = reinterpret_cast<float*>(at);
   a.group = Divisor(x.hq / x.hk), a.q_splits = Divisor(p.q_splits), a.q_chunk = p.q_chunk, a.k_splits = Divisor(p.k_splits), a.k_chunk = p.k_chunk;
