@@ -452,15 +452,11 @@ __device__ __forceinline__ void fold_items(const Args& a, unsigned block, int gr
   if (live && at.group == 0) store_four(static_cast<T*>(a.dw) + item * a.d, sum, 4 * at.t, a.d, a.quads);
 }
 
-// Both gradients in one launch (neither needs the other): `item_blocks` workgroups hold items, the others rows.  At the largest width,
-// where either's operands fill the registers, a launch each.
-constexpr int kItems = 1, kRowsOf = 2;
-template <typename T, int D, int STEP, int SIDES>
+// Both gradients in one launch (neither needs the other): `item_blocks` workgroups hold items, the others rows.
+template <typename T, int D, int STEP>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void catalogue_gradients_kernel(Args a, unsigned item_blocks) {
   extern __shared__ __align__(1024) unsigned char smem[];  // [2] stages
-  if constexpr (SIDES == kItems) items_gradient<T, D, STEP>(a, blockIdx.x, smem);
-  else if constexpr (SIDES == kRowsOf) rows_gradient<T, D, STEP>(a, blockIdx.x, smem);
-  else if (blockIdx.x < item_blocks) items_gradient<T, D, STEP>(a, blockIdx.x, smem);
+  if (blockIdx.x < item_blocks) items_gradient<T, D, STEP>(a, blockIdx.x, smem);
   else rows_gradient<T, D, STEP>(a, blockIdx.x - item_blocks, smem);
 }
 template <typename T, int D>
@@ -557,18 +553,8 @@ hipError_t backward(const Args& a, hipStream_t s) {
   if (hipError_t e = gather<T, true>(a, s); e != hipSuccess) return e;
   const int64_t item_blocks = a.dw ? (static_cast<int64_t>(a.items) + 127) / 128 * a.item_splits : 0, row_blocks = a.dx ? (a.rows + 127) / 128 * a.splits : 0;
   constexpr int lds = 2 * (Tile<T, D, STEP>::kBytes + 1024);
-  if constexpr (D < kMaxCatalogueWidth) {
-    static PerDevice granted;
-    if (hipError_t e = launch(granted, catalogue_gradients_kernel<T, D, STEP, kItems + kRowsOf>, item_blocks + row_blocks, lds, s, a, static_cast<unsigned>(item_blocks));
-        e != hipSuccess)
-      return e;
-  } else {
-    static PerDevice items_granted, rows_granted;
-    if (item_blocks > 0)
-      if (hipError_t e = launch(items_granted, catalogue_gradients_kernel<T, D, STEP, kItems>, item_blocks, lds, s, a, 0u); e != hipSuccess) return e;
-    if (row_blocks > 0)
-      if (hipError_t e = launch(rows_granted, catalogue_gradients_kernel<T, D, STEP, kRowsOf>, row_blocks, lds, s, a, 0u); e != hipSuccess) return e;
-  }
+  static PerDevice granted;
+  if (hipError_t e = launch(granted, catalogue_gradients_kernel<T, D, STEP>, item_blocks + row_blocks, lds, s, a, static_cast<unsigned>(item_blocks)); e != hipSuccess) return e;
   const int item_groups = fold_groups(a.item_splits, D / 4), row_groups = fold_groups(a.splits, D / 4);
   auto folds = [](int64_t rows, int groups) { const int64_t per = 256 / (D / 4) / groups; return (rows + per - 1) / per; };
   const int64_t item_folds = a.dw && a.item_splits > 1 ? folds(a.items, item_groups) : 0, row_folds = a.dx ? folds(a.rows, row_groups) : 0;
