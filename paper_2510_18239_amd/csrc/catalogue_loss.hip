@@ -142,11 +142,11 @@ __device__ __forceinline__ int list_rows(const Args& a, int first, int lane, int
 // Running maximum and sum of a chunk of the catalogue for 32 rows a wave.
 template <typename T, int D, int STEP>
 __global__ __launch_bounds__(256) void catalogue_lse_kernel(Args a) {
-  using Shape = Tile<T, D, STEP>;
+  using Stage = Stages<T, D, STEP, 1>;
   using Loader = TileLoader<T, D, STEP, 4>;
   using Reader = TileReader<T, D, STEP>;
   constexpr int VB = STEP / 32, NK = D / 16;
-  extern __shared__ __align__(1024) unsigned char smem[];  // [2] tiles
+  extern __shared__ __align__(1024) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);
   const int split = blockIdx.x % a.splits, tile = blockIdx.x / a.splits, row = tile * 128 + 32 * wave + n;
@@ -155,10 +155,10 @@ __global__ __launch_bounds__(256) void catalogue_lse_kernel(Args a) {
   const Rows wm{static_cast<const T*>(a.w) + static_cast<int64_t>(v0) * a.d, width, width, a.w_pieces};
   Loader wl;
   wl.init(wm, tid);
-  wl.issue(wm, 0, v1 - v0, smem, tid);
+  wl.issue(wm, 0, v1 - v0, Stage::tile(smem, 0, 0), tid);
   int count, from = 0;
   if (a.rows <= kFewRows) {
-    int32_t* places = reinterpret_cast<int32_t*>(smem + Shape::kBytes) + 32 * wave;  // (where the second tile will be)
+    int32_t* places = reinterpret_cast<int32_t*>(smem + Stage::kTiles) + 32 * wave;  // (where the first step's tile does not arrive)
     count = list_rows(a, row - n, lane, places, split == 0 && tile == 0 && wave == 0);
     if (row < count) from = places[n];
     if (split == 0 && g == 0 && row < count) a.live[1 + row] = from;
@@ -201,10 +201,9 @@ __global__ __launch_bounds__(256) void catalogue_lse_kernel(Args a) {
 #pragma unroll
   for (int e = 0; e < 16; ++e) before[e] = -INFINITY;
   auto arrived = [&](int i) -> unsigned {  // step i's tile; the next is asked for (past the last: nothing but zeros)
-    wait_lds_loads<0>();
-    lds_barrier();
-    wl.issue(wm, (i + 1) * STEP, v1 - v0, smem + (i + 1) % 2 * Shape::kBytes, tid);
-    return lds_offset_of(smem + i % 2 * Shape::kBytes);
+    Stage::template arrive<4>(smem, tid);
+    wl.issue(wm, (i + 1) * STEP, v1 - v0, Stage::tile(smem, i + 1, 0), tid);
+    return Stage::operand(smem, i, 0);
   };
   const int whole = (v1 - v0) / STEP;
   for (int i = 0; i < whole; ++i) {
@@ -225,7 +224,7 @@ __global__ __launch_bounds__(256) void catalogue_lse_kernel(Args a) {
 #pragma unroll 1
     for (int vb = 0; vb < VB; ++vb) {
       absorb(before);
-      before = logits(wt + 32 * vb * Shape::kRowBytes, 0);
+      before = logits(wt + 32 * vb * Reader::kRowBytes, 0);
 #pragma unroll
       for (int e = 0; e < 16; ++e)
         if (v0 + whole * STEP + 32 * vb + block_row(e, g) >= v1) before[e] = -INFINITY;
@@ -270,7 +269,7 @@ __global__ __launch_bounds__(256) void catalogue_loss_kernel(Args a) {
 // sum_v p_iv W_v over a chunk of the catalogue, 32 rows a wave.
 template <typename T, int D, int STEP>
 __device__ __forceinline__ void rows_gradient(Args a, unsigned block, unsigned char* smem) {
-  using Shape = Tile<T, D, STEP>;
+  using Stage = Stages<T, D, STEP, 1>;
   using Loader = TileLoader<T, D, STEP, 4>;
   using Reader = TileReader<T, D, STEP>;
   constexpr int VB = STEP / 32, NK = D / 16, OB = D / 32;
@@ -284,7 +283,7 @@ __device__ __forceinline__ void rows_gradient(Args a, unsigned block, unsigned c
   const Rows wm{static_cast<const T*>(a.w) + static_cast<int64_t>(v0) * a.d, width, width, a.w_pieces};
   Loader wl;
   wl.init(wm, tid);
-  wl.issue(wm, 0, v1 - v0, smem, tid);
+  wl.issue(wm, 0, v1 - v0, Stage::tile(smem, 0, 0), tid);
   Fragment<T> x[NK];
   load_row<T, D>(static_cast<const T*>(a.x) + static_cast<int64_t>(row < count ? a.live[1 + row] : 0) * a.d, width, a.x_pieces, row < count, g, x);
   const float c = a.scale * kLog2e, lse2 = row < count ? a.c_lse2[row] : 0.f;
@@ -292,10 +291,9 @@ __device__ __forceinline__ void rows_gradient(Args a, unsigned block, unsigned c
 #pragma unroll
   for (int ob = 0; ob < OB; ++ob) dx[ob] = zero_block();
   for (int i = 0; i < steps; ++i) {
-    wait_lds_loads<0>();
-    lds_barrier();
-    if (i + 1 < steps) wl.issue(wm, (i + 1) * STEP, v1 - v0, smem + (i + 1) % 2 * Shape::kBytes, tid);
-    const unsigned wt = lds_offset_of(smem + i % 2 * Shape::kBytes);
+    Stage::template arrive<4>(smem, tid);
+    if (i + 1 < steps) wl.issue(wm, (i + 1) * STEP, v1 - v0, Stage::tile(smem, i + 1, 0), tid);
+    const unsigned wt = Stage::operand(smem, i, 0);
 #pragma unroll
     for (int vb = 0; vb < VB; ++vb) {
       f32x16 p = zero_block();
@@ -342,10 +340,10 @@ __device__ __forceinline__ void fold_rows(const Args& a, unsigned block, int gro
 // sum_i e_iv X_i over a chunk of the listed rows, 32 items a wave.
 template <typename T, int D, int STEP>
 __device__ __forceinline__ void items_gradient(Args a, unsigned block, unsigned char* smem) {
-  using Shape = Tile<T, D, STEP>;
+  using Stage = Stages<T, D, STEP, 1, 4>;  // rows; lse2, dloss scale, target's place, its e
   using Loader = TileLoader<T, D, STEP, 4>;
   using Reader = TileReader<T, D, STEP>;
-  constexpr int RB = STEP / 32, NK = D / 16, OB = D / 32, kStage = Shape::kBytes + 1024;  // rows; lse2, dloss scale, target's place, its e, each [64]
+  constexpr int RB = STEP / 32, NK = D / 16, OB = D / 32;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);
   const int split = block % a.item_splits, tile = block / a.item_splits, count = a.live[0];
@@ -356,11 +354,10 @@ __device__ __forceinline__ void items_gradient(Args a, unsigned block, unsigned 
   Loader xl;
   xl.init(xm, tid);
   auto ask = [&](int i) {
-    unsigned char* at = smem + i % 2 * kStage;
-    xl.issue(xm, i * STEP, i1 - i0, at, tid);
+    xl.issue(xm, i * STEP, i1 - i0, Stage::tile(smem, i, 0), tid);
     const int from = i0 + i * STEP;
     const void* words[4] = {a.c_lse2, a.c_g, a.c_place, a.c_e};
-    words_to_lds(static_cast<const float*>(words[wave]) + from, min(STEP, i1 - from), at + Shape::kBytes + 256 * wave, lane);
+    words_to_lds(static_cast<const float*>(words[wave]) + from, min(STEP, i1 - from), Stage::words(smem, i, wave), lane);
   };
   if (steps > 0) ask(0);
   Fragment<T> w[NK];
@@ -370,19 +367,16 @@ __device__ __forceinline__ void items_gradient(Args a, unsigned block, unsigned 
 #pragma unroll
   for (int ob = 0; ob < OB; ++ob) dw[ob] = zero_block();
   for (int i = 0; i < steps; ++i) {
-    wait_lds_loads<0>();
-    lds_barrier();
+    Stage::template arrive<4>(smem, tid);
     if (i + 1 < steps) ask(i + 1);
-    const unsigned char* rows = smem + i % 2 * kStage;
-    const unsigned xt = lds_offset_of(rows);
-    const float *lse2 = reinterpret_cast<const float*>(rows + Shape::kBytes), *weight = lse2 + 64;
-    const int32_t* target = reinterpret_cast<const int32_t*>(weight + 64);
-    const float* own = weight + 128;
+    const unsigned xt = Stage::operand(smem, i, 0);
+    const float *lse2 = Stage::words(smem, i, 0), *weight = Stage::words(smem, i, 1), *own = Stage::words(smem, i, 3);
+    const int32_t* target = reinterpret_cast<const int32_t*>(Stage::words(smem, i, 2));
     // which of the step's rows have one of the wave's items for their target (rows past the last: with the weight 0)
     const unsigned long long chosen = __ballot(lane < STEP && static_cast<unsigned>(target[lane % STEP] - place0) < 32u);
 #pragma unroll(D < 256 ? RB : 1)
     for (int rb = 0; rb < RB; ++rb) {
-      const unsigned block = xt + 32 * rb * Shape::kRowBytes;
+      const unsigned block = xt + 32 * rb * Reader::kRowBytes;
       f32x16 e = zero_block();
 #pragma unroll
       for (int kk = 0; kk < NK; ++kk) e = mma16(read.row(block, 0, kk), w[kk], e);
@@ -427,7 +421,7 @@ __device__ __forceinline__ void items_gradient(Args a, unsigned block, unsigned 
             low[4 * j + y] = static_cast<__bf16>(t4[y] == place ? o4[y] - static_cast<float>(static_cast<__bf16>(o4[y])) : 0.f);
         }
 #pragma unroll
-        for (int ob = 0; ob < OB; ++ob) dw[ob] = mma16(read.column(xt + 16 * k * Shape::kRowBytes, 0, 32 * ob), low, dw[ob]);
+        for (int ob = 0; ob < OB; ++ob) dw[ob] = mma16(read.column(xt + 16 * k * Reader::kRowBytes, 0, 32 * ob), low, dw[ob]);
       }
     }
   }
@@ -455,7 +449,7 @@ __device__ __forceinline__ void fold_items(const Args& a, unsigned block, int gr
 // Both gradients in one launch (neither needs the other): `item_blocks` workgroups hold items, the others rows.
 template <typename T, int D, int STEP>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void catalogue_gradients_kernel(Args a, unsigned item_blocks) {
-  extern __shared__ __align__(1024) unsigned char smem[];  // [2] stages
+  extern __shared__ __align__(1024) unsigned char smem[];
   if (blockIdx.x < item_blocks) items_gradient<T, D, STEP>(a, blockIdx.x, smem);
   else rows_gradient<T, D, STEP>(a, blockIdx.x - item_blocks, smem);
 }
@@ -542,7 +536,7 @@ hipError_t forward(const Args& a, hipStream_t s) {
   if (a.rows > kFewRows)
     if (hipError_t e = gather<T, false>(a, s); e != hipSuccess) return e;
   static PerDevice granted;
-  if (hipError_t e = launch(granted, catalogue_lse_kernel<T, D, STEP>, (a.rows + 127) / 128 * a.splits, 2 * Tile<T, D, STEP>::kBytes, s, a); e != hipSuccess) return e;
+  if (hipError_t e = launch(granted, catalogue_lse_kernel<T, D, STEP>, (a.rows + 127) / 128 * a.splits, Stages<T, D, STEP, 1>::kBytes, s, a); e != hipSuccess) return e;
   hipLaunchKernelGGL(catalogue_loss_kernel<T>, dim3(static_cast<unsigned>((a.rows + 3) / 4)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
@@ -552,7 +546,7 @@ hipError_t backward(const Args& a, hipStream_t s) {
   constexpr int STEP = sizeof(T) == 2 ? 64 : 32;
   if (hipError_t e = gather<T, true>(a, s); e != hipSuccess) return e;
   const int64_t item_blocks = a.dw ? (static_cast<int64_t>(a.items) + 127) / 128 * a.item_splits : 0, row_blocks = a.dx ? (a.rows + 127) / 128 * a.splits : 0;
-  constexpr int lds = 2 * (Tile<T, D, STEP>::kBytes + 1024);
+  constexpr int lds = Stages<T, D, STEP, 1, 4>::kBytes;
   static PerDevice granted;
   if (hipError_t e = launch(granted, catalogue_gradients_kernel<T, D, STEP>, item_blocks + row_blocks, lds, s, a, static_cast<unsigned>(item_blocks)); e != hipSuccess) return e;
   const int item_groups = fold_groups(a.item_splits, D / 4), row_groups = fold_groups(a.splits, D / 4);

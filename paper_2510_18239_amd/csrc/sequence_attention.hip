@@ -30,14 +30,14 @@ struct Args {
 // this (a factor of 2^8 in p, which neither fp32 sums nor the rounding of p mind): rarely after a row's first tiles.
 constexpr float kHeadroom = 8.f;
 
-// WAVES waves of 32 rows each; KEYS keys a step, two steps' tiles in LDS (one in use, the other on its way).
+// WAVES waves of 32 rows each; KEYS keys a step.
 template <typename T, int DH, int WAVES, int KEYS>
 __global__ __launch_bounds__(WAVES * 64) void sequence_attention_kernel(Args a) {
-  using Shape = Tile<T, DH, KEYS>;
+  using Stage = Stages<T, DH, KEYS, 2>;  // keys, values
   using Loader = TileLoader<T, DH, KEYS, WAVES>;
   using Reader = TileReader<T, DH, KEYS>;
   constexpr int KB = KEYS / 32, OB = DH / 32, NK = DH / 16, ROWS = 32 * WAVES;
-  extern __shared__ __align__(1024) unsigned char smem[];  // [2][keys, values]
+  extern __shared__ __align__(1024) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);
   // last tiles of rows first: under a causal mask the longest
@@ -66,10 +66,9 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_kernel(Args a) 
   const Rows km{kp, static_cast<unsigned>(a.k_stride * sizeof(T)), width, a.pieces}, vm{vp, static_cast<unsigned>(a.v_stride * sizeof(T)), width, a.pieces};
   Loader kl, vl;
   kl.init(km, tid), vl.init(vm, tid);
-  auto stage = [&](int i) { return smem + i % 2 * 2 * Shape::kBytes; };
   auto ask = [&](int i) {
-    kl.issue(km, i * KEYS, k_end - k_begin, stage(i), tid);
-    vl.issue(vm, i * KEYS, k_end - k_begin, stage(i) + Shape::kBytes, tid);
+    kl.issue(km, i * KEYS, k_end - k_begin, Stage::tile(smem, i, 0), tid);
+    vl.issue(vm, i * KEYS, k_end - k_begin, Stage::tile(smem, i, 1), tid);
   };
   if (steps > 0) ask(0);
 
@@ -86,12 +85,11 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_kernel(Args a) 
   float m = -INFINITY, l = 0.f;  // of this lane's row; l of the lane half's keys
 
   for (int i = 0; i < steps; ++i) {
-    wait_lds_loads<0>();
-    lds_barrier();  // everyone's part of this step's tiles is there, and everyone is done with the last step's
+    Stage::template arrive<WAVES>(smem, tid);
     if (i + 1 < steps) ask(i + 1);
     const int key0 = k_begin + i * KEYS;
     if (key0 >= wave_most) continue;
-    const unsigned kt = lds_offset_of(stage(i)), vt = kt + Shape::kBytes;
+    const unsigned kt = Stage::operand(smem, i, 0), vt = Stage::operand(smem, i, 1);
     f32x16 s[KB];
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
@@ -239,7 +237,7 @@ Plan plan_of(const SequenceAttention& a) {
 
 template <typename T, int DH, int WAVES, int KEYS>
 hipError_t launch(const Args& a, hipStream_t s) {
-  constexpr int lds = 4 * Tile<T, DH, KEYS>::kBytes;
+  constexpr int lds = Stages<T, DH, KEYS, 2>::kBytes;
   static PerDevice granted;
   const auto kernel = sequence_attention_kernel<T, DH, WAVES, KEYS>;
   if (hipError_t e = allow_lds(granted, reinterpret_cast<const void*>(kernel), lds); e != hipSuccess) return e;

@@ -32,11 +32,11 @@ struct Args {
 
 template <typename T, int DH, int WAVES, int KEYS>
 __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args a) {
-  using Shape = Tile<T, DH, KEYS>;
+  using Stage = Stages<T, DH, KEYS, 2>;  // keys, values
   using Loader = TileLoader<T, DH, KEYS, WAVES>;
   using Reader = TileReader<T, DH, KEYS>;
   constexpr int KB = KEYS / 32, OB = DH / 32, NK = DH / 16, ROWS = 32 * WAVES;
-  extern __shared__ __align__(1024) unsigned char smem[];  // [2][keys, values]
+  extern __shared__ __align__(1024) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);
   const auto [b, kv, pair] = pair_of(a.deal);
@@ -61,9 +61,8 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
   Loader kl, vl;
   kl.init(km, tid), vl.init(vm, tid);
   auto ask = [&](int i) {
-    unsigned char* at = smem + i % 2 * 2 * Shape::kBytes;
-    kl.issue(km, i * KEYS, k_end - k_begin, at, tid);
-    vl.issue(vm, i * KEYS, k_end - k_begin, at + Shape::kBytes, tid);
+    kl.issue(km, i * KEYS, k_end - k_begin, Stage::tile(smem, i, 0), tid);
+    vl.issue(vm, i * KEYS, k_end - k_begin, Stage::tile(smem, i, 1), tid);
   };
   // Few keys: all their tiles fit, and D comes from its other form, sum_j p_ij <G_i, V_j>.  <G_i, O_i> carries the rounding of O to
   // the storage type, which is as large as the difference e_ij where a row sees two keys and fades with the square root of their
@@ -82,7 +81,7 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
     wait_lds_loads<0>();
     lds_barrier();
     for (int kb = 0; kb < KB * steps; ++kb) {
-      const unsigned kt = lds_offset_of(smem + kb / KB * 2 * Shape::kBytes) + kb % KB * 32 * Shape::kRowBytes, vt = kt + Shape::kBytes;
+      const unsigned rows = kb % KB * 32 * Reader::kRowBytes, kt = Stage::operand(smem, kb / KB, 0) + rows, vt = Stage::operand(smem, kb / KB, 1) + rows;
       f32x16 s = zero_block(), e = zero_block();
 #pragma unroll
       for (int kk = 0; kk < NK; ++kk) {
@@ -114,12 +113,11 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
   for (int x = 0; x < 16; ++x) less[x] = -delta;
 
   for (int i = 0; i < steps; ++i) {
-    wait_lds_loads<0>();
-    lds_barrier();
+    Stage::template arrive<WAVES>(smem, tid);
     if (i + 1 < steps && !resident) ask(i + 1);
     const int key0 = k_begin + i * KEYS;
     if (key0 >= wave_most) continue;
-    const unsigned kt = lds_offset_of(smem + i % 2 * 2 * Shape::kBytes), vt = kt + Shape::kBytes;
+    const unsigned kt = Stage::operand(smem, i, 0), vt = Stage::operand(smem, i, 1);
     const bool partial = key0 + KEYS > wave_least;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
@@ -159,12 +157,11 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
 
 template <typename T, int DH, int STEP>
 __global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
-  using Shape = Tile<T, DH, STEP>;
+  using Stage = Stages<T, DH, STEP, 2, 2>;  // queries, output gradients; lse2, -D
   using Loader = TileLoader<T, DH, STEP, 4>;
   using Reader = TileReader<T, DH, STEP>;
   constexpr int QB = STEP / 32, OB = DH / 32, NK = DH / 16, KEYS = 128;
-  constexpr int kStage = 2 * Shape::kBytes + 512;          // queries, output gradients, lse2 [64], -D [64]
-  extern __shared__ __align__(1024) unsigned char smem[];  // [2] stages
+  extern __shared__ __align__(1024) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);
   // first keys first: under a causal mask most queries see them
@@ -193,13 +190,12 @@ __global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
   int ask_head = each ? begin_step / each : 0, ask_at = each ? begin_step % each * STEP : 0, at = ask_at;  // at: this step's first query, from `begin`
   qm.base = static_cast<const char*>(qm.base) + ask_head * width, gm.base = static_cast<const char*>(gm.base) + ask_head * width;
   auto ask = [&](int i) {
-    unsigned char* to = smem + i % 2 * kStage;
     const int count = qs.used - begin - ask_at;
-    ql.issue(qm, ask_at, qs.used - begin, to, tid);
-    gl.issue(gm, ask_at, qs.used - begin, to + Shape::kBytes, tid);
+    ql.issue(qm, ask_at, qs.used - begin, Stage::tile(smem, i, 0), tid);
+    gl.issue(gm, ask_at, qs.used - begin, Stage::tile(smem, i, 1), tid);
     if (wave < 2) {
       const float* from = (wave == 0 ? a.lse2 : a.less) + (kv * group + ask_head) * static_cast<int64_t>(a.where.q_rows) + qs.start + begin + ask_at;
-      words_to_lds(from, min(count, STEP), reinterpret_cast<float*>(to + 2 * Shape::kBytes) + 64 * wave, lane);
+      words_to_lds(from, min(count, STEP), Stage::words(smem, i, wave), lane);
     }
     ask_at += STEP;
     if (ask_at >= each * STEP) {
@@ -218,15 +214,13 @@ __global__ __launch_bounds__(256) void sequence_attention_dkv_kernel(Args a) {
   for (int ob = 0; ob < OB; ++ob) dk[ob] = dv[ob] = zero_block();
 
   for (int i = 0; i < steps; ++i) {
-    wait_lds_loads<0>();
-    lds_barrier();
+    Stage::template arrive<4>(smem, tid);
     if (i + 1 < steps) ask(i + 1);
     const int q0 = begin + at;
     at = at + STEP < each * STEP ? at + STEP : 0;
     if (q0 + STEP <= wave_first) continue;
-    const unsigned char* tiles = smem + i % 2 * kStage;
-    const unsigned qt = lds_offset_of(tiles), gt = qt + Shape::kBytes;
-    const float *lse2 = reinterpret_cast<const float*>(tiles + 2 * Shape::kBytes), *less = lse2 + 64;
+    const unsigned qt = Stage::operand(smem, i, 0), gt = Stage::operand(smem, i, 1);
+    const float *lse2 = Stage::words(smem, i, 0), *less = Stage::words(smem, i, 1);
     const bool partial = q0 < wave_all || q0 + STEP > qs.used;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
@@ -342,7 +336,7 @@ hipError_t run(Args a, const Plan& p, int users, hipStream_t s) {
   constexpr int STEP = sizeof(T) == 2 ? 64 : 32;
   const int max_q = a.where.max_q, max_k = a.where.max_k;
   if (max_q > 0) {
-    constexpr int lds = 4 * Tile<T, DH, STEP>::kBytes;
+    constexpr int lds = Stages<T, DH, STEP, 2>::kBytes;
     static PerDevice granted;
     const auto kernel = sequence_attention_dq_kernel<T, DH, 4, STEP>;
     if (hipError_t e = allow_lds(granted, reinterpret_cast<const void*>(kernel), lds); e != hipSuccess) return e;
@@ -351,7 +345,7 @@ hipError_t run(Args a, const Plan& p, int users, hipStream_t s) {
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
   if (max_k > 0) {
-    constexpr int lds = 2 * (2 * Tile<T, DH, STEP>::kBytes + 512);
+    constexpr int lds = Stages<T, DH, STEP, 2, 2>::kBytes;
     static PerDevice granted;
     const auto kernel = sequence_attention_dkv_kernel<T, DH, STEP>;
     if (hipError_t e = allow_lds(granted, reinterpret_cast<const void*>(kernel), lds); e != hipSuccess) return e;
