@@ -202,6 +202,10 @@ __global__ __launch_bounds__(256) void sequence_attention_merge_kernel(Args a, i
   if (a.lse != nullptr && at.t == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
+// Keys a step of four waves: as many as leave a compute unit four workgroups' registers and LDS.  (Up to 256 events of 64 users, d/h = 32:
+// 8.9 us in steps of 64 keys, 8.5 of 128; 16 of 2048 to 4096 events, d/h = 64: 113 and 122.)
+constexpr int keys_of(bool bf16, int dh) { return !bf16 ? 32 : dh <= 32 ? 128 : 64; }
+
 struct Plan {
   int waves, keys, tiles, splits, chunk, dh;  // dh: padded
   size_t o_bytes, bytes;
@@ -212,19 +216,19 @@ struct Plan {
 // and to end: so eight waves a compute unit are wanted, of four steps at least, but no more than 256 chunks of a row, which have to be
 // folded again.  (32 users, up to 4096 keys: 14.6 us in chunks of 128 keys, 15.8 of 256; four users of up to 131072: 53 us in 512 chunks,
 // 49 in 256.  More tiles in flight take the LDS of the other waves: three 16.0, four 15.7 and 51.9.)  Of workgroups of four waves, two a
-// compute unit, of four steps at least.  (8 users' up to 64 new events over up to 8192 keys: 17.6 us, 19.0 with one workgroup a unit or
-// eight steps, 23 with four and two steps; five users' up to 501 events in fp32: 21.2 us, 24.5 with eight steps.)
+// compute unit, of 256 keys at least (fp32: 128).  (8 users' up to 64 new events over up to 8192 keys: 17.6 us, 19.0 with one workgroup a unit or
+// 512 keys, 23 with four and 128; five users' up to 501 events in fp32: 21.2 us, 24.5 with 256.)
 Plan plan_of(const SequenceAttention& a) {
   const int64_t B = a.B, hk = a.hk, max_k = std::max(a.max_k, 1), rows = std::max<int64_t>(a.max_q, 1) * (a.hq / a.hk);
   const int dh = a.dh, dtype = a.dtype;
   Plan p{};
   p.dh = dh <= 32 ? 32 : dh <= 64 ? 64 : 128;
   p.waves = rows <= 32 ? 1 : 4;
-  p.keys = dtype == 1 && p.waves > 1 ? 64 : 32;
+  p.keys = p.waves > 1 ? keys_of(dtype == 1, p.dh) : 32;
   p.tiles = static_cast<int>((rows + 32 * p.waves - 1) / (32 * p.waves));
   const int64_t groups = B * hk * p.tiles;
   const int64_t want = (p.waves == 1 ? 8 : 2) * static_cast<int64_t>(compute_units());
-  const int64_t least = p.waves == 1 ? std::max<int64_t>(128, (max_k + 255) / 256) : 4 * p.keys;
+  const int64_t least = p.waves == 1 ? std::max<int64_t>(128, (max_k + 255) / 256) : dtype == 1 ? 256 : 128;
   int64_t splits = groups >= want ? 1 : std::min((want + groups - 1) / groups, (max_k + least - 1) / least);
   int64_t chunk = (max_k + splits - 1) / splits;
   chunk = (chunk + p.keys - 1) / p.keys * p.keys;
@@ -250,7 +254,7 @@ hipError_t launch(const Args& a, hipStream_t s) {
 
 template <typename T, int DH>
 hipError_t run(const Args& a, const Plan& p, hipStream_t s) {
-  constexpr int KEYS = sizeof(T) == 2 ? 64 : 32;
+  constexpr int KEYS = keys_of(sizeof(T) == 2, DH);
   hipError_t e = p.waves == 1 ? launch<T, DH, 1, 32>(a, s) : launch<T, DH, 4, KEYS>(a, s);
   if (e != hipSuccess || a.splits.d == 1) return e;
   const int groups = fold_groups(a.splits.d, DH / 4);
