@@ -313,20 +313,23 @@ struct Plan {
 };
 
 // Two workgroups of four waves a compute unit are wanted; no chunk is shorter than 256 keys (bf16; 128: fp32), or four steps over queries.
+// Of ragged users twice as many for the kernel that holds keys: its workgroups are few, and the longest user's first keys see all of that
+// user's queries of all heads of the group.  (Four users of 79 to 3983 events, eight heads on two, d/h = 80: 775 us with two a unit, 553
+// with four; 52 of up to 551, eight heads on one, 122 and 103; 16 of 3129 each 314 and 342; in fp32, where a unit holds one, 162 and 177.)
 Plan plan_of(const SequenceAttention& a) {
   const int64_t group = a.hq / a.hk, pairs = static_cast<int64_t>(a.B) * a.hk, max_q = std::max(a.max_q, 1), max_k = std::max(a.max_k, 1);
   const int64_t want = 2 * static_cast<int64_t>(compute_units()), step = a.dtype == 1 ? 64 : 32;
   Plan p{};
   p.dh = a.dh <= 32 ? 32 : a.dh <= 64 ? 64 : 128;
   p.q_tiles = static_cast<int>((max_q * group + 127) / 128), p.k_tiles = static_cast<int>((max_k + 127) / 128);
-  auto cut = [&](int64_t tiles, int64_t length, int64_t least, int& splits, int& chunk) {
-    const int64_t most = std::max<int64_t>(1, (length + least - 1) / least), n = std::min(most, std::max<int64_t>(1, want / (pairs * tiles)));
+  auto cut = [&](int64_t tiles, int64_t length, int64_t least, int64_t want, int& splits, int& chunk) {
+    const int64_t most = std::max<int64_t>(1, (length + least - 1) / least), n = std::min(most, std::max<int64_t>(1, (want + pairs * tiles - 1) / (pairs * tiles)));
     const int64_t c = ((length + n - 1) / n + step - 1) / step * step;
     chunk = static_cast<int>(std::min<int64_t>(c, (int64_t{1} << 31) - 1)), splits = static_cast<int>((length + c - 1) / c);
   };
-  cut(p.q_tiles, max_k, 4 * step, p.q_splits, p.q_chunk);
+  cut(p.q_tiles, max_k, 4 * step, want, p.q_splits, p.q_chunk);
   const int64_t steps = (max_q + step - 1) / step * group;
-  cut(p.k_tiles, steps * step, 4 * step, p.k_splits, p.k_chunk);
+  cut(p.k_tiles, steps * step, 4 * step, ragged(a) && a.dtype == 1 ? 2 * want : want, p.k_splits, p.k_chunk);
   p.k_chunk = static_cast<int>((p.k_chunk + step - 1) / step);
   p.stats = align_up(static_cast<size_t>(a.q_rows) * a.hq * sizeof(float));
   p.part_q = p.q_splits > 1 ? align_up(static_cast<size_t>(p.q_splits) * a.q_rows * a.hq * p.dh * sizeof(float)) : 0;
@@ -374,7 +377,7 @@ bool sequence_attention_backward_fits(const SequenceAttention& a) {  // 2^32 wor
   if (rows >= (int64_t{1} << 31) - 128 || pairs >= (int64_t{1} << 24)) return false;
   const Plan p = plan_of(a);
   const int64_t q_deep = static_cast<int64_t>(p.q_tiles) * p.q_splits, k_deep = static_cast<int64_t>(p.k_tiles) * p.k_splits;
-  // (of a side that is cut, users times heads times rows are less than 2^17: a side with more has workgroups enough)
+  // (of a side that is cut, users times heads times rows are less than 2^18: a side with more has workgroups enough)
   return q_deep < 65536 && k_deep < 65536 && pairs * q_deep < (int64_t{1} << 24) && pairs * k_deep < (int64_t{1} << 24);
 }
 
@@ -387,7 +390,7 @@ hipError_t sequence_attention_backward(const SequenceAttention& x, void* workspa
   a.q = x.Q, a.k = x.K, a.v = x.V, a.o = x.O, a.go = x.dO, a.dq = x.dQ, a.dk = x.dK, a.dv = x.dV, a.lse = x.lse;
   a.q_stride = x.q_stride, a.k_stride = x.k_stride, a.v_stride = x.v_stride;
   a.dq_stride = x.dq_stride, a.dk_stride = x.dk_stride, a.dv_stride = x.dv_stride;
-  a.where = Packing(x), a.deal = Deal(x, std::max(p.q_splits, p.k_splits));
+  a.where = Packing(x), a.deal = Deal(x, true);
   char* at = static_cast<char*>(workspace);
   a.lse2 = reinterpret_cast<float*>(at), at += p.stats;
   a.less = reinterpret_cast<float*>(at), at += p.stats;

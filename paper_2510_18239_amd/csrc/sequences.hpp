@@ -45,21 +45,21 @@ __device__ __forceinline__ Spans spans_of(const Packing& p, int b) {
 // where users times key heads is a multiple of eight a pair's tiles all land on one XCD and read its keys from one L2: right where all
 // histories are as long, but where they are not the XCD with the longest users ends last.  Then every second tile moves on to the next
 // pair's place.  (16 users of 2048 to 4096 events, two key heads: forward 131 -> 114 us; 16 of 4096: 159, and 165 if they moved.)
-// Chunks of one row's keys stay, for the merge that reads their states from the same L2.
+inline bool ragged(const SequenceAttention& x) {
+  return x.q_lens != nullptr || x.k_lens != nullptr || x.k_rows < static_cast<int64_t>(x.B) * x.max_k || x.q_rows < static_cast<int64_t>(x.B) * x.max_q;
+}
 struct Deal {
   Divisor pairs, hk;
-  bool ragged;
+  bool moves;
   Deal() = default;
-  Deal(const SequenceAttention& x, int splits)
-      : pairs(static_cast<uint32_t>(x.B) * x.hk), hk(x.hk),
-        ragged(splits == 1 && (x.q_lens != nullptr || x.k_lens != nullptr || x.k_rows < static_cast<int64_t>(x.B) * x.max_k || x.q_rows < static_cast<int64_t>(x.B) * x.max_q)) {}
+  Deal(const SequenceAttention& x, bool may_move) : pairs(static_cast<uint32_t>(x.B) * x.hk), hk(x.hk), moves(may_move && ragged(x)) {}
 };
 struct Pair {
   int b, kv, index;
 };
 __device__ __forceinline__ Pair pair_of(const Deal& d) {
   const int hk = d.hk.d, pair = blockIdx.y * hk + blockIdx.x;
-  if (!d.ragged) return {static_cast<int>(blockIdx.y), static_cast<int>(blockIdx.x), pair};
+  if (!d.moves) return {static_cast<int>(blockIdx.y), static_cast<int>(blockIdx.x), pair};
   const int moved = pair + blockIdx.z / 2, at = moved - d.pairs.divide(moved) * d.pairs.d, b = d.hk.divide(at);
   return {b, at - b * hk, at};
 }
