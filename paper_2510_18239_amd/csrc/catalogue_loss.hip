@@ -49,27 +49,36 @@ __device__ __forceinline__ int place_of(const Args& a, int item) {
   return (item - at * static_cast<int>(a.item_tiles.d)) * 128 + at;
 }
 
-constexpr int kGatherRows = 64;  // rows a workgroup of the gather takes at a time
+constexpr int kGatherRows = 64, kGatherWaves = 16;  // rows a workgroup of the gather takes at a time
 
 // Lists the rows with a target.  Every workgroup counts all targets by itself (they are few next to the products), so that no
-// workgroup waits for another.
+// workgroup waits for another: large workgroups, one a compute unit, because they all read all targets.
 template <typename T, bool BACKWARD>
-__global__ __launch_bounds__(256) void gather_kernel(Args a, int64_t each) {
-  __shared__ int sums[4][2];
+__global__ __launch_bounds__(64 * kGatherWaves) void gather_kernel(Args a, int64_t each) {
+  __shared__ int sums[kGatherWaves][2];
   __shared__ int place[kGatherRows];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t begin = blockIdx.x * each, end = min(begin + each, a.rows);
-  auto has = [&](int64_t i) { return static_cast<unsigned>(a.targets[i]) < static_cast<unsigned>(a.items); };
+  auto named = [&](int target) { return static_cast<unsigned>(target) < static_cast<unsigned>(a.items); };
+  auto has = [&](int64_t i) { return named(a.targets[i]); };
   int before = 0, all = 0;
-#pragma unroll 8
-  for (int64_t i = tid; i < a.rows; i += 256) {
-    const int x = has(i);
+  auto count = [&](int64_t i, int target) {
+    const int x = named(target);
     all += x, before += i < begin ? x : 0;
+  };
+  const int64_t fours = reinterpret_cast<uintptr_t>(a.targets) % 16 == 0 ? a.rows / 4 : 0;
+#pragma unroll 4
+  for (int64_t i = tid; i < fours; i += 64 * kGatherWaves) {
+    const i32x4 t = reinterpret_cast<const i32x4*>(a.targets)[i];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) count(4 * i + j, t[j]);
   }
+  for (int64_t i = 4 * fours + tid; i < a.rows; i += 64 * kGatherWaves) count(i, a.targets[i]);
   for (int o = 32; o; o >>= 1) before += __shfl_xor(before, o, 64), all += __shfl_xor(all, o, 64);
   if (lane == 0) sums[wave][0] = before, sums[wave][1] = all;
   __syncthreads();
-  before = sums[0][0] + sums[1][0] + sums[2][0] + sums[3][0], all = sums[0][1] + sums[1][1] + sums[2][1] + sums[3][1];
+  before = all = 0;
+  for (int w = 0; w < kGatherWaves; ++w) before += sums[w][0], all += sums[w][1];
   if (blockIdx.x == 0 && tid == 0) a.live[0] = all;
   const bool whole = all == a.rows;
   for (int64_t at = begin; at < end; at += kGatherRows) {
@@ -91,7 +100,7 @@ __global__ __launch_bounds__(256) void gather_kernel(Args a, int64_t each) {
     __syncthreads();
     const int here = static_cast<int>(min<int64_t>(kGatherRows, end - at));
 #pragma unroll 4
-    for (int r = wave; r < here; r += 4) {  // a wave a row
+    for (int r = wave; r < here; r += kGatherWaves) {  // a wave a row
       const T* from = static_cast<const T*>(a.x) + (at + r) * a.d;
       const int to = place[r];
       if (to >= 0) {  // e of the row's own target, dloss scale (p - 1)
@@ -128,15 +137,21 @@ __global__ __launch_bounds__(256) void gather_kernel(Args a, int64_t each) {
 constexpr int kFewRows = 4096;
 __device__ __forceinline__ int list_rows(const Args& a, int first, int lane, int32_t* places, bool zero_others) {
   int before = 0;
-#pragma unroll 4
-  for (int base = 0; base < a.rows; base += 64) {
-    const int i = base + lane;
-    const bool x = i < a.rows && static_cast<unsigned>(a.targets[i]) < static_cast<unsigned>(a.items);
-    const unsigned long long votes = __ballot(x);
-    const int to = before + __popcll(votes & ((1ull << lane) - 1)) - first;
-    if (x && static_cast<unsigned>(to) < 32u) places[to] = i;
-    if (zero_others && !x && i < a.rows) a.loss[i] = 0.f, a.lse[i] = 0.f;
-    before += __popcll(votes);
+  const int rows = static_cast<int>(a.rows);
+  for (int base = 0; base < rows; base += 512) {
+    int target[8];  // loads in flight
+#pragma unroll
+    for (int j = 0; j < 8; ++j) target[j] = a.targets[min(base + 64 * j + lane, rows - 1)];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int i = base + 64 * j + lane;
+      const bool x = i < rows && static_cast<unsigned>(target[j]) < static_cast<unsigned>(a.items);
+      const unsigned long long votes = __ballot(x);
+      const int to = before + __popcll(votes & ((1ull << lane) - 1)) - first;
+      if (x && static_cast<unsigned>(to) < 32u) places[to] = i;
+      if (zero_others && !x && i < rows) a.loss[i] = 0.f, a.lse[i] = 0.f;
+      before += __popcll(votes);
+    }
   }
   wave_lds_fence();
   return before;
@@ -521,8 +536,8 @@ Args args_of(const CatalogueLoss& x, const Plan& p, void* workspace) {
 
 template <typename T, bool BACKWARD>
 hipError_t gather(const Args& a, hipStream_t s) {
-  const int64_t each = std::max<int64_t>(16, (a.rows + 1023) / 1024);
-  hipLaunchKernelGGL((gather_kernel<T, BACKWARD>), dim3(static_cast<unsigned>((a.rows + each - 1) / each)), dim3(256), 0, s, a, each);
+  const int64_t each = std::max<int64_t>(16, (a.rows + compute_units() - 1) / compute_units());
+  hipLaunchKernelGGL((gather_kernel<T, BACKWARD>), dim3(static_cast<unsigned>((a.rows + each - 1) / each)), dim3(64 * kGatherWaves), 0, s, a, each);
   return hipGetLastError();
 }
 
