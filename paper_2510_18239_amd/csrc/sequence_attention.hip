@@ -213,8 +213,9 @@ struct Plan {
 
 // Rows that one wave holds take a workgroup of one wave.  Where the tiles of rows are too few to fill the chip, the keys are cut
 // into chunks as well.  A lone wave needs about 1600 cycles for a step of 32 keys, most of them waiting for itself, and 4600 to start
-// and to end: so eight waves a compute unit are wanted, of four steps at least, but no more than 256 chunks of a row, which have to be
-// folded again.  (32 users, up to 4096 keys: 14.6 us in chunks of 128 keys, 15.8 of 256; four users of up to 131072: 53 us in 512 chunks,
+// and to end: so eight waves a compute unit are wanted, of four steps at least (fp32, where a step takes 4 us at d/h = 128: of one), but no
+// more than 256 chunks of a row, which have to be folded again.  (32 users, up to 4096 keys: 14.6 us in chunks of 128 keys, 15.8 of 256; fp32, two users, up to 249 keys: 27.9 us and
+// 12.5 in chunks of 32; four users of up to 131072: 53 us in 512 chunks,
 // 49 in 256.  More tiles in flight take the LDS of the other waves: three 16.0, four 15.7 and 51.9.)  Of workgroups of four waves, two a
 // compute unit, of 256 keys at least (fp32: 128).  (8 users' up to 64 new events over up to 8192 keys: 17.6 us, 19.0 with one workgroup a unit or
 // 512 keys, 23 with four and 128; five users' up to 501 events in fp32: 21.2 us, 24.5 with 256.)
@@ -228,7 +229,7 @@ Plan plan_of(const SequenceAttention& a) {
   p.tiles = static_cast<int>((rows + 32 * p.waves - 1) / (32 * p.waves));
   const int64_t groups = B * hk * p.tiles;
   const int64_t want = (p.waves == 1 ? 8 : 2) * static_cast<int64_t>(compute_units());
-  const int64_t least = p.waves == 1 ? std::max<int64_t>(128, (max_k + 255) / 256) : dtype == 1 ? 256 : 128;
+  const int64_t least = p.waves == 1 ? std::max<int64_t>(dtype == 1 ? 128 : 32, (max_k + 255) / 256) : dtype == 1 ? 256 : 128;
   int64_t splits = groups >= want ? 1 : std::min((want + groups - 1) / groups, (max_k + least - 1) / least);
   int64_t chunk = (max_k + splits - 1) / splits;
   chunk = (chunk + p.keys - 1) / p.keys * p.keys;
