@@ -372,7 +372,7 @@ int32_t lime_scores(const lime_scoring_model* model, const void* E, const int32_
  * lime_sequence_attention_backward - dQ, dK, dV from dO and the forward pass's inputs and outputs O, lse (same sizes, same
  *   `where`).  dQ, dK, dV have strides of their own (they may be columns of one wider gradient); gradients of a key head are summed
  *   over its query heads.  Rows of a slot not in use get zeros, rows outside all slots are left as they were.
- *   Workspace of both: lime_sequence_attention_workspace_bytes.
+ *   Workspace of both: lime_sequence_attention_workspace_bytes of the same `where` (how the work is cut depends on whether lens are given).
  *
  * lime_catalogue_loss - softmax cross entropy of rows against a catalogue of items, the logits never in memory:
  *     z_iv = scale <X_i, W_v>,   lse_i = log sum_v exp(z_iv),   loss_i = lse_i - z_{i,targets[i]}.

@@ -287,9 +287,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void sequence_attentio
 
 // The chunks' sums folded: of dQ by the first q_blocks workgroups of a user where its keys were cut, then of dK and dV where the queries were.
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void sequence_attention_fold_kernel(Args a, unsigned q_blocks, int groups) {
-  const Folder<DH> at(groups);
+__global__ __launch_bounds__(256) void sequence_attention_fold_kernel(Args a, unsigned q_blocks, int q_groups, int k_groups) {
   const bool of_q = blockIdx.x < q_blocks;
+  const int groups = of_q ? q_groups : k_groups;
+  const Folder<DH> at(groups);
   const int block = of_q ? blockIdx.x : blockIdx.x - q_blocks, heads = of_q ? a.hq : a.hk, each = of_q ? heads : 2 * heads;
   const int tile = block / each, h = block - tile * each, what = of_q ? 0 : h < heads ? 1 : 2, head = what == 2 ? h - heads : h;
   const int b = blockIdx.y, i = tile * at.rows + at.row, splits = of_q ? a.q_splits.d : a.k_splits.d;
@@ -361,10 +362,10 @@ hipError_t run(Args a, const Plan& p, int users, hipStream_t s) {
   }
   const bool q_folds = p.q_splits > 1 && max_q > 0, k_folds = p.k_splits > 1 && max_k > 0;
   if (!q_folds && !k_folds) return hipSuccess;
-  const int groups = fold_groups(std::max(q_folds ? p.q_splits : 1, k_folds ? p.k_splits : 1), DH / 4), per = 256 / (DH / 4) / groups;
-  auto blocks = [&](int rows, int heads) { return static_cast<unsigned>((rows + per - 1) / per * heads); };
-  const unsigned q_blocks = q_folds ? blocks(max_q, a.hq) : 0, k_blocks = k_folds ? blocks(max_k, 2 * a.hk) : 0;
-  hipLaunchKernelGGL((sequence_attention_fold_kernel<T, DH>), dim3(q_blocks + k_blocks, users), dim3(256), 0, s, a, q_blocks, groups);
+  const int q_groups = fold_groups(p.q_splits, DH / 4), k_groups = fold_groups(p.k_splits, DH / 4);
+  auto blocks = [](int rows, int groups, int heads) { const int per = 256 / (DH / 4) / groups; return static_cast<unsigned>((rows + per - 1) / per * heads); };
+  const unsigned q_blocks = q_folds ? blocks(max_q, q_groups, a.hq) : 0, k_blocks = k_folds ? blocks(max_k, k_groups, 2 * a.hk) : 0;
+  hipLaunchKernelGGL((sequence_attention_fold_kernel<T, DH>), dim3(q_blocks + k_blocks, users), dim3(256), 0, s, a, q_blocks, q_groups, k_groups);
   return hipGetLastError();
 }
 
