@@ -178,6 +178,8 @@ def test_histories(dtype, lens, hq, hk, dh):
     ([50, 9], [20, 0], (60, 30), 2, 1, 64, True),                # more queries than keys: the first see nothing
     ([50, 9, 33], [20, 0, 200], (60, 210), 2, 1, 48, False),     # every key for every query
     ([128, 127], [400, 129], (130, 401), 1, 1, 32, False),
+    ([1, 1, 0, 1, 1, 1, 1, 1], [900, 3, 700, 0, 256, 257, 64, 800], (1, 900), 4, 2, 64, True),  # chunks of sixteen pairs, which change places
+    ([1, 1, 1, 1], [3000, 40, 1, 2222], (1, 3000), 16, 2, 100, True),
 ])
 def test_slots_and_lengths(dtype, q_lens, k_lens, slots, hq, hk, dh, causal):
     attention_case(dtype, q_lens, k_lens, hq, hk, dh, causal, slots)
@@ -281,11 +283,11 @@ def test_a_cache_whose_offsets_pass_32_bits():
 
 
 # ------------------------------------------------------------------------------------------------- the loss
-def loss_case(dtype, rows, items, d, unlabelled, scale=None, std=1.0, shift=0.0, seed=0):
+def loss_case(dtype, rows, items, d, unlabelled, scale=None, std=1.0, shift=0.0, seed=0, below=None):
     u, scale = U[dtype], d**-0.5 if scale is None else scale
     (x, X), (w, W) = make((rows, d), dtype, seed, std, shift), make((items, d), dtype, seed + 1, 1.0, -shift)
     r = np.random.default_rng(seed + 2)
-    t = r.integers(0, items, rows)
+    t = r.integers(0, below or items, rows)
     none = r.random(rows) < unlabelled
     t[none] = r.choice([-1, -100, items, 2**31 - 1, -(2**31)], none.sum())
     x[torch.from_numpy(none).cuda()] = float("nan")  # a row without a target may hold anything
@@ -324,6 +326,24 @@ def test_loss(dtype, rows, items, d, unlabelled):
 def test_loss_scales(dtype, scale, std, shift):
     """Equal logits; negative scales; sharp softmaxes; logits all near -250, whose exponentials alone would not be numbers."""
     loss_case(dtype, 90, 777, 64, 0.1, scale, std, shift)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,items,d,below", [(500, 1000, 64, 1), (700, 2000, 256, 8), (6000, 300, 32, 2)])
+def test_loss_of_popular_items(dtype, rows, items, d, below):
+    loss_case(dtype, rows, items, d, 0.1, below=below)
+
+
+@pytest.mark.parametrize("rows", [1, 300, 5003])
+def test_targets_that_are_not_aligned(rows):
+    (x, _), (w, _) = make((rows, 64), "bf16", 0), make((400, 64), "bf16", 1)
+    t = ints(np.random.default_rng(2).integers(-50, 400, rows + 1))
+    g = torch.ones(rows, device="cuda")
+    at = [t[1:], t[1:].clone()]
+    assert at[0].data_ptr() % 16 == 4 and at[1].data_ptr() % 16 == 0
+    loss = [binding.lime_catalogue_loss(x, w, t) for t in at]
+    assert same(*loss)
+    assert same(*(binding.lime_catalogue_loss_backward(g, x, w, t, loss[0][1]) for t in at))
 
 
 def test_rows_of_the_loss_that_are_not_finite_stay_alone():
