@@ -213,12 +213,12 @@ struct Plan {
 
 // Rows that one wave holds take a workgroup of one wave.  Where the tiles of rows are too few to fill the chip, the keys are cut
 // into chunks as well.  A lone wave needs about 1600 cycles for a step of 32 keys, most of them waiting for itself, and 4600 to start
-// and to end: so eight waves a compute unit are wanted, of four steps at least (fp32, where a step takes 4 us at d/h = 128: of one), but no
-// more than 256 chunks of a row, which have to be folded again.  (32 users, up to 4096 keys: 14.6 us in chunks of 128 keys, 15.8 of 256; fp32, two users, up to 249 keys: 27.9 us and
-// 12.5 in chunks of 32; four users of up to 131072: 53 us in 512 chunks,
-// 49 in 256.  More tiles in flight take the LDS of the other waves: three 16.0, four 15.7 and 51.9.)  Of workgroups of four waves, two a
-// compute unit, of 256 keys at least (fp32: 128).  (8 users' up to 64 new events over up to 8192 keys: 17.6 us, 19.0 with one workgroup a unit or
-// 512 keys, 23 with four and 128; five users' up to 501 events in fp32: 21.2 us, 24.5 with 256.)
+// and to end: so eight waves a compute unit are wanted, of four steps at least (fp32, where a step takes 4 us at d/h = 128: of one), but
+// no more than 256 chunks of a row, which have to be folded again.  (32 users, up to 4096 keys: 14.6 us in chunks of 128 keys, 15.8 of
+// 256; four users of up to 131072: 53 us in 512 chunks, 49 in 256; fp32, two users, up to 249 keys: 27.9 us in chunks of 128, 12.5 of
+// 32.  More tiles in flight take the LDS of the other waves: three 16.0, four 15.7 and 51.9.)  Of workgroups of four waves, two a
+// compute unit, of 256 keys at least (fp32: 128).  (8 users' up to 64 new events over up to 8192 keys: 17.6 us, 19.0 with one workgroup
+// a unit or 512 keys, 23 with four and 128; five users' up to 501 events in fp32: 21.2 us, 24.5 with 256.)
 Plan plan_of(const SequenceAttention& a) {
   const int64_t B = a.B, hk = a.hk, max_k = std::max(a.max_k, 1), rows = std::max<int64_t>(a.max_q, 1) * (a.hq / a.hk);
   const int dh = a.dh, dtype = a.dtype;
