@@ -478,7 +478,7 @@ __global__ __launch_bounds__(256) void catalogue_fold_kernel(Args a, unsigned it
   else fold_rows<T, D>(a, blockIdx.x - item_blocks, row_groups);
 }
 
-int padded(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
+int padded(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
 // The streamed side cut into chunks so that the workgroups fill the chip: `tiles` of the side that stays, `length` of the other.
 // But a chunk's sums, `floats` of them, are written and read again at some 4.5 TB/s: no more chunks than the square root of the steps' time
@@ -595,16 +595,16 @@ hipError_t catalogue_loss(const CatalogueLoss& x, void* workspace, hipStream_t s
   const Plan p = plan_of(x.rows, x.items, x.d, x.dtype, false);
   const Args a = args_of(x, p, workspace);
   const int D = padded(x.d);
-  if (x.dtype == 1) return D == 64 ? forward<bf16_t, 64>(a, s) : D == 128 ? forward<bf16_t, 128>(a, s) : forward<bf16_t, 256>(a, s);
-  return D == 64 ? forward<float, 64>(a, s) : D == 128 ? forward<float, 128>(a, s) : forward<float, 256>(a, s);
+  if (x.dtype == 1) return D == 32 ? forward<bf16_t, 32>(a, s) : D == 64 ? forward<bf16_t, 64>(a, s) : D == 128 ? forward<bf16_t, 128>(a, s) : forward<bf16_t, 256>(a, s);
+  return D == 32 ? forward<float, 32>(a, s) : D == 64 ? forward<float, 64>(a, s) : D == 128 ? forward<float, 128>(a, s) : forward<float, 256>(a, s);
 }
 
 hipError_t catalogue_loss_backward(const CatalogueLoss& x, void* workspace, hipStream_t s) {
   const Plan p = plan_of(x.rows, x.items, x.d, x.dtype, true);
   const Args a = args_of(x, p, workspace);
   const int D = padded(x.d);
-  if (x.dtype == 1) return D == 64 ? backward<bf16_t, 64>(a, s) : D == 128 ? backward<bf16_t, 128>(a, s) : backward<bf16_t, 256>(a, s);
-  return D == 64 ? backward<float, 64>(a, s) : D == 128 ? backward<float, 128>(a, s) : backward<float, 256>(a, s);
+  if (x.dtype == 1) return D == 32 ? backward<bf16_t, 32>(a, s) : D == 64 ? backward<bf16_t, 64>(a, s) : D == 128 ? backward<bf16_t, 128>(a, s) : backward<bf16_t, 256>(a, s);
+  return D == 32 ? backward<float, 32>(a, s) : D == 64 ? backward<float, 64>(a, s) : D == 128 ? backward<float, 128>(a, s) : backward<float, 256>(a, s);
 }
 
 }  // namespace lime
