@@ -481,9 +481,10 @@ __global__ __launch_bounds__(256) void catalogue_fold_kernel(Args a, unsigned it
 int padded(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
 // The streamed side cut into chunks so that the workgroups fill the chip: `tiles` of the side that stays, `length` of the other.
-// But a chunk's sums, `floats` of them, are written and read again at some 4.5 TB/s: no more chunks than the square root of the steps' time
-// over that of one chunk's sums, where the two times' sum is least.  (A step takes about D / 128 us in bf16, half as long again in fp32.
-// 12093 rows over 293 items, d = 256: 82 us with a chunk for every step, 68 so; 1003 over 20011 in fp32 142 and 132.)
+// But a chunk's sums, `floats` of them, are written and read again at some 4.5 TB/s: no more chunks than the square root of the steps'
+// time over that of one chunk's sums, where the two times' sum is least, rounded down unless near the next.  (A step takes about
+// D / 128 us in bf16, half as long again in fp32.  12093 rows over 293 items, d = 256: 82 us with a chunk for every step, 68 so; 1003
+// over 20011 in fp32 142 and 132.)
 struct Cut {
   int splits, chunk;
 };
@@ -491,7 +492,7 @@ Cut cut(int64_t tiles, int64_t length, int step, int64_t want, int64_t floats, d
   int64_t splits = tiles >= want ? 1 : (want + tiles - 1) / tiles;
   const int64_t steps = (length + step - 1) / step;
   const double sums_us = floats * 8 / 4.5e6, least = std::sqrt(steps * step_us / sums_us);
-  splits = std::max<int64_t>(1, std::min({splits, steps, static_cast<int64_t>(std::min(least + 0.5, 1e6))}));
+  splits = std::max<int64_t>(1, std::min({splits, steps, static_cast<int64_t>(std::min(least + 0.2, 1e6))}));
   int64_t chunk = (length + splits - 1) / splits;
   chunk = (chunk + step - 1) / step * step;
   return {static_cast<int>((length + chunk - 1) / chunk), static_cast<int>(chunk)};
@@ -504,7 +505,8 @@ struct Plan {
 Plan plan_of(int64_t rows, int items, int d, int dtype, bool backward) {
   Plan p{};
   const int step = dtype == 1 ? 64 : 32, D = padded(d);
-  const int64_t want = 2 * static_cast<int64_t>(compute_units());
+  // (up to 64 columns leave a unit the registers of four workgroups: 20000 rows over 20000 items, d = 64, 369 us with two, 325 with four)
+  const int64_t want = (D <= 64 ? 4 : 2) * static_cast<int64_t>(compute_units());
   const double step_us = D / 128. * (dtype == 1 ? 1 : 1.5);
   p.rows = cut((rows + 127) / 128, items, step, want, rows * (backward ? D : 2), step_us);
   p.items = cut((static_cast<int64_t>(items) + 127) / 128, rows, step, want, static_cast<int64_t>(items) * D, step_us);
