@@ -50,6 +50,9 @@ __device__ __forceinline__ int place_of(const Args& a, int item) {
   return (item - at * static_cast<int>(a.item_tiles.d)) * 128 + at;
 }
 
+// Tiles and chunks' sums are as wide as a power of two; products are done for the first C columns, a multiple of 32, of the tiles.
+constexpr int tile_width(int c) { return c <= 32 ? 32 : c <= 64 ? 64 : c <= 128 ? 128 : 256; }
+
 constexpr int kGatherRows = 64, kGatherWaves = 16;  // rows a workgroup of the gather takes at a time
 
 // Lists the rows with a target.  Every workgroup counts all targets by itself (they are few next to the products), so that no
@@ -159,12 +162,13 @@ __device__ __forceinline__ int list_rows(const Args& a, int first, int lane, int
 }
 
 // Running maximum and sum of a chunk of the catalogue for 32 rows a wave.
-template <typename T, int D, int STEP>
+template <typename T, int C, int STEP>
 __global__ __launch_bounds__(256) void catalogue_lse_kernel(Args a) {
+  constexpr int D = tile_width(C);
   using Stage = Stages<T, D, STEP, 1>;
   using Loader = TileLoader<T, D, STEP, 4>;
   using Reader = TileReader<T, D, STEP>;
-  constexpr int VB = STEP / 32, NK = D / 16;
+  constexpr int VB = STEP / 32, NK = C / 16;
   extern __shared__ __align__(1024) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);
@@ -191,7 +195,7 @@ __global__ __launch_bounds__(256) void catalogue_lse_kernel(Args a) {
     return;
   }
   Fragment<T> x[NK];
-  load_row<T, D>(static_cast<const T*>(a.x) + static_cast<int64_t>(from) * a.d, width, a.x_pieces, row < count, g, x);
+  load_row<T, C>(static_cast<const T*>(a.x) + static_cast<int64_t>(from) * a.d, width, a.x_pieces, row < count, g, x);
   const float c = fmaxf(fabsf(a.scale) * kLog2e, 1e-37f);
   if (a.scale < 0.f) {
 #pragma unroll
@@ -286,12 +290,13 @@ __global__ __launch_bounds__(256) void catalogue_loss_kernel(Args a) {
 }
 
 // sum_v p_iv W_v over a chunk of the catalogue, 32 rows a wave.
-template <typename T, int D, int STEP>
+template <typename T, int C, int STEP>
 __device__ __forceinline__ void rows_gradient(Args a, unsigned block, unsigned char* smem) {
+  constexpr int D = tile_width(C);
   using Stage = Stages<T, D, STEP, 1>;
   using Loader = TileLoader<T, D, STEP, 4>;
   using Reader = TileReader<T, D, STEP>;
-  constexpr int VB = STEP / 32, NK = D / 16, OB = D / 32;
+  constexpr int VB = STEP / 32, NK = C / 16, OB = C / 32;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);
   const int split = block % a.splits, tile = block / a.splits, count = a.live[0];
@@ -304,7 +309,7 @@ __device__ __forceinline__ void rows_gradient(Args a, unsigned block, unsigned c
   wl.init(wm, tid);
   wl.issue(wm, 0, v1 - v0, Stage::tile(smem, 0, 0), tid);
   Fragment<T> x[NK];
-  load_row<T, D>(static_cast<const T*>(a.x) + static_cast<int64_t>(row < count ? a.live[1 + row] : 0) * a.d, width, a.x_pieces, row < count, g, x);
+  load_row<T, C>(static_cast<const T*>(a.x) + static_cast<int64_t>(row < count ? a.live[1 + row] : 0) * a.d, width, a.x_pieces, row < count, g, x);
   const float c = a.scale * kLog2e, lse2 = row < count ? a.c_lse2[row] : 0.f;
   f32x16 dx[OB];
 #pragma unroll
@@ -357,12 +362,13 @@ __device__ __forceinline__ void fold_rows(const Args& a, unsigned block, int gro
 }
 
 // sum_i e_iv X_i over a chunk of the listed rows, 32 items a wave.
-template <typename T, int D, int STEP>
+template <typename T, int C, int STEP>
 __device__ __forceinline__ void items_gradient(Args a, unsigned block, unsigned char* smem) {
+  constexpr int D = tile_width(C);
   using Stage = Stages<T, D, STEP, 1, 4>;  // rows; lse2, dloss scale, target's place, its e
   using Loader = TileLoader<T, D, STEP, 4>;
   using Reader = TileReader<T, D, STEP>;
-  constexpr int RB = STEP / 32, NK = D / 16, OB = D / 32;
+  constexpr int RB = STEP / 32, NK = C / 16, OB = C / 32;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);
   const int split = block % a.item_splits, tile = block / a.item_splits, count = a.live[0];
@@ -380,7 +386,7 @@ __device__ __forceinline__ void items_gradient(Args a, unsigned block, unsigned 
   };
   if (steps > 0) ask(0);
   Fragment<T> w[NK];
-  load_row<T, D>(static_cast<const T*>(a.w) + static_cast<int64_t>(item) * a.d, width, a.w_pieces, item < a.items, g, w);
+  load_row<T, C>(static_cast<const T*>(a.w) + static_cast<int64_t>(item) * a.d, width, a.w_pieces, item < a.items, g, w);
   const float c = a.scale * kLog2e;
   f32x16 dw[OB];
 #pragma unroll
@@ -466,11 +472,11 @@ __device__ __forceinline__ void fold_items(const Args& a, unsigned block, int gr
 }
 
 // Both gradients in one launch (neither needs the other): `item_blocks` workgroups hold items, the others rows.
-template <typename T, int D, int STEP>
+template <typename T, int C, int STEP>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void catalogue_gradients_kernel(Args a, unsigned item_blocks) {
   extern __shared__ __align__(1024) unsigned char smem[];
-  if (blockIdx.x < item_blocks) items_gradient<T, D, STEP>(a, blockIdx.x, smem);
-  else rows_gradient<T, D, STEP>(a, blockIdx.x - item_blocks, smem);
+  if (blockIdx.x < item_blocks) items_gradient<T, C, STEP>(a, blockIdx.x, smem);
+  else rows_gradient<T, C, STEP>(a, blockIdx.x - item_blocks, smem);
 }
 template <typename T, int D>
 __global__ __launch_bounds__(256) void catalogue_fold_kernel(Args a, unsigned item_blocks, int item_groups, int row_groups) {
@@ -478,7 +484,6 @@ __global__ __launch_bounds__(256) void catalogue_fold_kernel(Args a, unsigned it
   else fold_rows<T, D>(a, blockIdx.x - item_blocks, row_groups);
 }
 
-int padded(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
 // The streamed side cut into chunks so that the workgroups fill the chip: `tiles` of the side that stays, `length` of the other.
 // But a chunk's sums, `floats` of them, are written and read again at some 4.5 TB/s: no more chunks than the square root of the steps'
@@ -504,7 +509,7 @@ struct Plan {
 };
 Plan plan_of(int64_t rows, int items, int d, int dtype, bool backward) {
   Plan p{};
-  const int step = dtype == 1 ? 64 : 32, D = padded(d);
+  const int step = dtype == 1 ? 64 : 32, D = tile_width(d);
   // (up to 64 columns leave a unit the registers of four workgroups: 20000 rows over 20000 items, d = 64, 369 us with two, 325 with four)
   const int64_t want = (D <= 64 ? 4 : 2) * static_cast<int64_t>(compute_units());
   const double step_us = D / 128. * (dtype == 1 ? 1 : 1.5);
@@ -557,25 +562,27 @@ hipError_t launch(PerDevice& granted, K kernel, int64_t blocks, int lds, hipStre
   return hipGetLastError();
 }
 
-template <typename T, int D>
+template <typename T, int C>
 hipError_t forward(const Args& a, hipStream_t s) {
+  constexpr int D = tile_width(C);
   constexpr int STEP = sizeof(T) == 2 ? 64 : 32;
   if (a.rows > kFewRows)
     if (hipError_t e = gather<T, false>(a, s); e != hipSuccess) return e;
   static PerDevice granted;
-  if (hipError_t e = launch(granted, catalogue_lse_kernel<T, D, STEP>, (a.rows + 127) / 128 * a.splits, Stages<T, D, STEP, 1>::kBytes, s, a); e != hipSuccess) return e;
+  if (hipError_t e = launch(granted, catalogue_lse_kernel<T, C, STEP>, (a.rows + 127) / 128 * a.splits, Stages<T, D, STEP, 1>::kBytes, s, a); e != hipSuccess) return e;
   hipLaunchKernelGGL(catalogue_loss_kernel<T>, dim3(static_cast<unsigned>((a.rows + 3) / 4)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
-template <typename T, int D>
+template <typename T, int C>
 hipError_t backward(const Args& a, hipStream_t s) {
+  constexpr int D = tile_width(C);
   constexpr int STEP = sizeof(T) == 2 ? 64 : 32;
   if (hipError_t e = gather<T, true>(a, s); e != hipSuccess) return e;
   const int64_t item_blocks = a.dw ? (static_cast<int64_t>(a.items) + 127) / 128 * a.item_splits : 0, row_blocks = a.dx ? (a.rows + 127) / 128 * a.splits : 0;
   constexpr int lds = Stages<T, D, STEP, 1, 4>::kBytes;
   static PerDevice granted;
-  if (hipError_t e = launch(granted, catalogue_gradients_kernel<T, D, STEP>, item_blocks + row_blocks, lds, s, a, static_cast<unsigned>(item_blocks)); e != hipSuccess) return e;
+  if (hipError_t e = launch(granted, catalogue_gradients_kernel<T, C, STEP>, item_blocks + row_blocks, lds, s, a, static_cast<unsigned>(item_blocks)); e != hipSuccess) return e;
   const int item_groups = fold_groups(a.item_splits, D / 4), row_groups = fold_groups(a.splits, D / 4);
   auto folds = [](int64_t rows, int groups) { const int64_t per = 256 / (D / 4) / groups; return (rows + per - 1) / per; };
   const int64_t item_folds = a.dw && a.item_splits > 1 ? folds(a.items, item_groups) : 0, row_folds = a.dx ? folds(a.rows, row_groups) : 0;
@@ -583,6 +590,17 @@ hipError_t backward(const Args& a, hipStream_t s) {
   hipLaunchKernelGGL((catalogue_fold_kernel<T, D>), dim3(static_cast<unsigned>(item_folds + row_folds)), dim3(256), 0, s, a, static_cast<unsigned>(item_folds), item_groups,
                      row_groups);
   return hipGetLastError();
+}
+
+// f(width) for the narrowest width of products that holds d columns
+template <typename F>
+hipError_t at_width(int d, F f) {
+  if (d <= 32) return f(std::integral_constant<int, 32>{});
+  if (d <= 64) return f(std::integral_constant<int, 64>{});
+  if (d <= 96) return f(std::integral_constant<int, 96>{});
+  if (d <= 128) return f(std::integral_constant<int, 128>{});
+  if (d <= 224) return f(std::integral_constant<int, 224>{});
+  return f(std::integral_constant<int, 256>{});
 }
 
 }  // namespace
@@ -596,17 +614,13 @@ size_t catalogue_loss_workspace(int64_t rows, int items, int d, int dtype, bool 
 hipError_t catalogue_loss(const CatalogueLoss& x, void* workspace, hipStream_t s) {
   const Plan p = plan_of(x.rows, x.items, x.d, x.dtype, false);
   const Args a = args_of(x, p, workspace);
-  const int D = padded(x.d);
-  if (x.dtype == 1) return D == 32 ? forward<bf16_t, 32>(a, s) : D == 64 ? forward<bf16_t, 64>(a, s) : D == 128 ? forward<bf16_t, 128>(a, s) : forward<bf16_t, 256>(a, s);
-  return D == 32 ? forward<float, 32>(a, s) : D == 64 ? forward<float, 64>(a, s) : D == 128 ? forward<float, 128>(a, s) : forward<float, 256>(a, s);
+  return at_width(x.d, [&](auto width) { return x.dtype == 1 ? forward<bf16_t, width.value>(a, s) : forward<float, width.value>(a, s); });
 }
 
 hipError_t catalogue_loss_backward(const CatalogueLoss& x, void* workspace, hipStream_t s) {
   const Plan p = plan_of(x.rows, x.items, x.d, x.dtype, true);
   const Args a = args_of(x, p, workspace);
-  const int D = padded(x.d);
-  if (x.dtype == 1) return D == 32 ? backward<bf16_t, 32>(a, s) : D == 64 ? backward<bf16_t, 64>(a, s) : D == 128 ? backward<bf16_t, 128>(a, s) : backward<bf16_t, 256>(a, s);
-  return D == 32 ? backward<float, 32>(a, s) : D == 64 ? backward<float, 64>(a, s) : D == 128 ? backward<float, 128>(a, s) : backward<float, 256>(a, s);
+  return at_width(x.d, [&](auto width) { return x.dtype == 1 ? backward<bf16_t, width.value>(a, s) : backward<float, width.value>(a, s); });
 }
 
 }  // namespace lime
