@@ -50,9 +50,6 @@ __device__ __forceinline__ int place_of(const Args& a, int item) {
   return (item - at * static_cast<int>(a.item_tiles.d)) * 128 + at;
 }
 
-// Tiles and chunks' sums are as wide as a power of two; products are done for the first C columns, a multiple of 32, of the tiles.
-constexpr int tile_width(int c) { return c <= 32 ? 32 : c <= 64 ? 64 : c <= 128 ? 128 : 256; }
-
 constexpr int kGatherRows = 64, kGatherWaves = 16;  // rows a workgroup of the gather takes at a time
 
 // Lists the rows with a target.  Every workgroup counts all targets by itself (they are few next to the products), so that no

@@ -34,12 +34,13 @@ struct Args {
 constexpr float kHeadroom = 8.f;
 
 // WAVES waves of 32 rows each; KEYS keys a step.
-template <typename T, int DH, int WAVES, int KEYS>
+template <typename T, int C, int WAVES, int KEYS>
 __global__ __launch_bounds__(WAVES * 64) void sequence_attention_kernel(Args a) {
+  constexpr int DH = tile_width(C);
   using Stage = Stages<T, DH, KEYS, 2>;  // keys, values
   using Loader = TileLoader<T, DH, KEYS, WAVES>;
   using Reader = TileReader<T, DH, KEYS>;
-  constexpr int KB = KEYS / 32, OB = DH / 32, NK = DH / 16, ROWS = 32 * WAVES;
+  constexpr int KB = KEYS / 32, OB = C / 32, NK = C / 16, ROWS = 32 * WAVES;
   extern __shared__ __align__(1024) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);
@@ -77,7 +78,7 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_kernel(Args a) 
 
   Fragment<T> q[NK];
   const T* qp = static_cast<const T*>(a.q) + (qs.start + query) * a.q_stride + head * a.dh;
-  load_row<T, DH>(qp, width, a.pieces, live, g, q);
+  load_row<T, C>(qp, width, a.pieces, live, g, q);
   if (a.negate) {
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk) negate(q[kk]);
@@ -223,7 +224,7 @@ Plan plan_of(const SequenceAttention& a) {
   const int64_t B = a.B, hk = a.hk, max_k = std::max(a.max_k, 1), rows = std::max<int64_t>(a.max_q, 1) * (a.hq / a.hk);
   const int dh = a.dh, dtype = a.dtype;
   Plan p{};
-  p.dh = dh <= 32 ? 32 : dh <= 64 ? 64 : 128;
+  p.dh = tile_width(dh);
   p.waves = rows <= 32 ? 1 : 4;
   p.keys = p.waves > 1 ? keys_of(dtype == 1, p.dh) : 32;
   p.tiles = static_cast<int>((rows + 32 * p.waves - 1) / (32 * p.waves));
@@ -243,20 +244,21 @@ Plan plan_of(const SequenceAttention& a) {
   return p;
 }
 
-template <typename T, int DH, int WAVES, int KEYS>
+template <typename T, int C, int WAVES, int KEYS>
 hipError_t launch(const Args& a, hipStream_t s) {
+  constexpr int DH = tile_width(C);
   constexpr int lds = Stages<T, DH, KEYS, 2>::kBytes;
   static PerDevice granted;
-  const auto kernel = sequence_attention_kernel<T, DH, WAVES, KEYS>;
+  const auto kernel = sequence_attention_kernel<T, C, WAVES, KEYS>;
   if (hipError_t e = allow_lds(granted, reinterpret_cast<const void*>(kernel), lds); e != hipSuccess) return e;
   hipLaunchKernelGGL(kernel, dim3(a.hk, a.B, a.tiles * a.splits.d), dim3(WAVES * 64), lds, s, a);
   return hipGetLastError();
 }
 
-template <typename T, int DH>
+template <typename T, int C>
 hipError_t run(const Args& a, const Plan& p, hipStream_t s) {
-  constexpr int KEYS = keys_of(sizeof(T) == 2, DH);
-  hipError_t e = p.waves == 1 ? launch<T, DH, 1, 32>(a, s) : launch<T, DH, 4, KEYS>(a, s);
+  constexpr int DH = tile_width(C), KEYS = keys_of(sizeof(T) == 2, DH);
+  hipError_t e = p.waves == 1 ? launch<T, C, 1, 32>(a, s) : launch<T, C, 4, KEYS>(a, s);
   if (e != hipSuccess || a.splits.d == 1) return e;
   const int groups = fold_groups(a.splits.d, DH / 4);
   const int64_t rows = static_cast<int64_t>(a.where.max_q) * a.group.d, per = 256 / (DH / 4) / groups;
@@ -294,8 +296,7 @@ hipError_t sequence_attention(const SequenceAttention& x, void* workspace, hipSt
   a.pieces = multiple(x.Q, 16) && multiple(x.K, 16) && multiple(x.V, 16) && x.dh * e % 16 == 0 && x.q_stride * e % 16 == 0 &&
              x.k_stride * e % 16 == 0 && x.v_stride * e % 16 == 0;
   a.quads = x.dh % 4 == 0 && multiple(x.O, 4 * e);
-  if (x.dtype == 1) return p.dh == 32 ? run<bf16_t, 32>(a, p, s) : p.dh == 64 ? run<bf16_t, 64>(a, p, s) : run<bf16_t, 128>(a, p, s);
-  return p.dh == 32 ? run<float, 32>(a, p, s) : p.dh == 64 ? run<float, 64>(a, p, s) : run<float, 128>(a, p, s);
+  return at_head_width(x.dh, [&](auto width) { return x.dtype == 1 ? run<bf16_t, width.value>(a, p, s) : run<float, width.value>(a, p, s); });
 }
 
 }  // namespace lime

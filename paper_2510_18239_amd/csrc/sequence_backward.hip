@@ -32,12 +32,13 @@ struct Args {
   bool pieces, causal, quads;
 };
 
-template <typename T, int DH, int WAVES, int KEYS>
+template <typename T, int C, int WAVES, int KEYS>
 __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args a) {
+  constexpr int DH = tile_width(C);
   using Stage = Stages<T, DH, KEYS, 2>;  // keys, values
   using Loader = TileLoader<T, DH, KEYS, WAVES>;
   using Reader = TileReader<T, DH, KEYS>;
-  constexpr int KB = KEYS / 32, OB = DH / 32, NK = DH / 16, ROWS = 32 * WAVES;
+  constexpr int KB = KEYS / 32, OB = C / 32, NK = C / 16, ROWS = 32 * WAVES;
   extern __shared__ __align__(1024) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);
@@ -75,8 +76,8 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
 
   const int64_t row = (qs.start + query) * a.hq + head;
   Fragment<T> q[NK], go[NK];
-  load_row<T, DH>(static_cast<const T*>(a.q) + (qs.start + query) * a.q_stride + head * a.dh, width, a.pieces, live, g, q);
-  load_row<T, DH>(static_cast<const T*>(a.go) + row * a.dh, width, a.pieces, live, g, go);
+  load_row<T, C>(static_cast<const T*>(a.q) + (qs.start + query) * a.q_stride + head * a.dh, width, a.pieces, live, g, q);
+  load_row<T, C>(static_cast<const T*>(a.go) + row * a.dh, width, a.pieces, live, g, go);
   const float c = a.scale * kLog2e, lse2 = live ? a.lse[row] * kLog2e : 0.f;
   float delta = 0.f;
   if (resident) {
@@ -97,7 +98,7 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
     delta = pair_sum(delta);
   } else {
     Fragment<T> o[NK];
-    load_row<T, DH>(static_cast<const T*>(a.o) + row * a.dh, width, a.pieces, live, g, o);
+    load_row<T, C>(static_cast<const T*>(a.o) + row * a.dh, width, a.pieces, live, g, o);
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk)
 #pragma unroll
@@ -159,12 +160,13 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
 
 // (bf16, d/h = 128: kept to 256 registers, with eight of a wave's loaded again for every 32 queries, for a second wave a SIMD: 16 causal
 // histories of 4096 events 1150 us with one, 1030 with two.)
-template <typename T, int DH, int STEP>
+template <typename T, int C, int STEP>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void sequence_attention_dkv_kernel(Args a) {
+  constexpr int DH = tile_width(C);
   using Stage = Stages<T, DH, STEP, 2, 2>;  // queries, output gradients; lse2, -D
   using Loader = TileLoader<T, DH, STEP, 4>;
   using Reader = TileReader<T, DH, STEP>;
-  constexpr int QB = STEP / 32, OB = DH / 32, NK = DH / 16, KEYS = 128;
+  constexpr int QB = STEP / 32, OB = C / 32, NK = C / 16, KEYS = 128;
   extern __shared__ __align__(1024) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);
@@ -210,8 +212,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void sequence_attentio
   if (steps > 0) ask(0);
 
   Fragment<T> k[NK], v[NK];
-  load_row<T, DH>(static_cast<const T*>(a.k) + (ks.start + key) * a.k_stride + kv * a.dh, width, a.pieces, live, g, k);
-  load_row<T, DH>(static_cast<const T*>(a.v) + (ks.start + key) * a.v_stride + kv * a.dh, width, a.pieces, live, g, v);
+  load_row<T, C>(static_cast<const T*>(a.k) + (ks.start + key) * a.k_stride + kv * a.dh, width, a.pieces, live, g, k);
+  load_row<T, C>(static_cast<const T*>(a.v) + (ks.start + key) * a.v_stride + kv * a.dh, width, a.pieces, live, g, v);
   const float c = a.scale * kLog2e;
   f32x16 dk[OB], dv[OB];
 #pragma unroll
@@ -321,7 +323,7 @@ Plan plan_of(const SequenceAttention& a) {
   const int64_t group = a.hq / a.hk, pairs = static_cast<int64_t>(a.B) * a.hk, max_q = std::max(a.max_q, 1), max_k = std::max(a.max_k, 1);
   const int64_t want = 2 * static_cast<int64_t>(compute_units()), step = a.dtype == 1 ? 64 : 32;
   Plan p{};
-  p.dh = a.dh <= 32 ? 32 : a.dh <= 64 ? 64 : 128;
+  p.dh = tile_width(a.dh);
   p.q_tiles = static_cast<int>((max_q * group + 127) / 128), p.k_tiles = static_cast<int>((max_k + 127) / 128);
   auto cut = [&](int64_t tiles, int64_t length, int64_t least, int64_t want, int& splits, int& chunk) {
     const int64_t most = std::max<int64_t>(1, (length + least - 1) / least), n = std::min(most, std::max<int64_t>(1, (want + pairs * tiles - 1) / (pairs * tiles)));
@@ -339,14 +341,14 @@ Plan plan_of(const SequenceAttention& a) {
   return p;
 }
 
-template <typename T, int DH>
+template <typename T, int C>
 hipError_t run(Args a, const Plan& p, int users, hipStream_t s) {
-  constexpr int STEP = sizeof(T) == 2 ? 64 : 32;
+  constexpr int DH = tile_width(C), STEP = sizeof(T) == 2 ? 64 : 32;
   const int max_q = a.where.max_q, max_k = a.where.max_k;
   if (max_q > 0) {
     constexpr int lds = Stages<T, DH, STEP, 2>::kBytes;
     static PerDevice granted;
-    const auto kernel = sequence_attention_dq_kernel<T, DH, 4, STEP>;
+    const auto kernel = sequence_attention_dq_kernel<T, C, 4, STEP>;
     if (hipError_t e = allow_lds(granted, reinterpret_cast<const void*>(kernel), lds); e != hipSuccess) return e;
     a.tiles = p.q_tiles;
     hipLaunchKernelGGL(kernel, dim3(a.hk, users, p.q_tiles * p.q_splits), dim3(256), lds, s, a);
@@ -355,7 +357,7 @@ hipError_t run(Args a, const Plan& p, int users, hipStream_t s) {
   if (max_k > 0) {
     constexpr int lds = Stages<T, DH, STEP, 2, 2>::kBytes;
     static PerDevice granted;
-    const auto kernel = sequence_attention_dkv_kernel<T, DH, STEP>;
+    const auto kernel = sequence_attention_dkv_kernel<T, C, STEP>;
     if (hipError_t e = allow_lds(granted, reinterpret_cast<const void*>(kernel), lds); e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3(a.hk, users, p.k_tiles * p.k_splits), dim3(256), lds, s, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
@@ -404,8 +406,7 @@ hipError_t sequence_attention_backward(const SequenceAttention& x, void* workspa
              x.q_stride * e % 16 == 0 && x.k_stride * e % 16 == 0 && x.v_stride * e % 16 == 0;
   a.quads = x.dh % 4 == 0 && x.dq_stride % 4 == 0 && x.dk_stride % 4 == 0 && x.dv_stride % 4 == 0 && multiple(x.dQ, 4 * e) && multiple(x.dK, 4 * e) &&
             multiple(x.dV, 4 * e);
-  if (x.dtype == 1) return p.dh == 32 ? run<bf16_t, 32>(a, p, x.B, s) : p.dh == 64 ? run<bf16_t, 64>(a, p, x.B, s) : run<bf16_t, 128>(a, p, x.B, s);
-  return p.dh == 32 ? run<float, 32>(a, p, x.B, s) : p.dh == 64 ? run<float, 64>(a, p, x.B, s) : run<float, 128>(a, p, x.B, s);
+  return at_head_width(x.dh, [&](auto width) { return x.dtype == 1 ? run<bf16_t, width.value>(a, p, x.B, s) : run<float, width.value>(a, p, x.B, s); });
 }
 
 }  // namespace lime

@@ -64,6 +64,15 @@ __device__ __forceinline__ Pair pair_of(const Deal& d) {
   return {b, at - b * hk, at};
 }
 
+// f(width) for the narrowest width of products that holds heads of dh.
+template <typename F>
+hipError_t at_head_width(int dh, F f) {
+  if (dh <= 32) return f(std::integral_constant<int, 32>{});
+  if (dh <= 64) return f(std::integral_constant<int, 64>{});
+  if (dh <= 96) return f(std::integral_constant<int, 96>{});
+  return f(std::integral_constant<int, 128>{});
+}
+
 // How many keys query i of a user sees: all, or those up to its own place counted from the end.
 __device__ __forceinline__ int keys_seen(int i, int n_q, int n_k, bool causal) { return causal ? min(n_k, max(0, i + 1 + n_k - n_q)) : n_k; }
 
