@@ -40,7 +40,7 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_kernel(Args a) 
   using Stage = Stages<T, DH, KEYS, 2>;  // keys, values
   using Loader = TileLoader<T, DH, KEYS, WAVES>;
   using Reader = TileReader<T, DH, KEYS>;
-  constexpr int KB = KEYS / 32, OB = C / 32, NK = C / 16, ROWS = 32 * WAVES;
+  constexpr int KB = KEYS / 32, OB = (C + 31) / 32, NK = C / 16, ROWS = 32 * WAVES;
   extern __shared__ __align__(1024) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);

@@ -38,7 +38,7 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
   using Stage = Stages<T, DH, KEYS, 2>;  // keys, values
   using Loader = TileLoader<T, DH, KEYS, WAVES>;
   using Reader = TileReader<T, DH, KEYS>;
-  constexpr int KB = KEYS / 32, OB = C / 32, NK = C / 16, ROWS = 32 * WAVES;
+  constexpr int KB = KEYS / 32, OB = (C + 31) / 32, NK = C / 16, ROWS = 32 * WAVES;
   extern __shared__ __align__(1024) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);
@@ -166,7 +166,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void sequence_attentio
   using Stage = Stages<T, DH, STEP, 2, 2>;  // queries, output gradients; lse2, -D
   using Loader = TileLoader<T, DH, STEP, 4>;
   using Reader = TileReader<T, DH, STEP>;
-  constexpr int QB = STEP / 32, OB = C / 32, NK = C / 16, KEYS = 128;
+  constexpr int QB = STEP / 32, OB = (C + 31) / 32, NK = C / 16, KEYS = 128;
   extern __shared__ __align__(1024) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);

@@ -68,7 +68,9 @@ __device__ __forceinline__ Pair pair_of(const Deal& d) {
 template <typename F>
 hipError_t at_head_width(int dh, F f) {
   if (dh <= 32) return f(std::integral_constant<int, 32>{});
+  if (dh <= 48) return f(std::integral_constant<int, 48>{});
   if (dh <= 64) return f(std::integral_constant<int, 64>{});
+  if (dh <= 80) return f(std::integral_constant<int, 80>{});
   if (dh <= 96) return f(std::integral_constant<int, 96>{});
   return f(std::integral_constant<int, 128>{});
 }
