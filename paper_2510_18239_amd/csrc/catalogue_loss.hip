@@ -339,7 +339,7 @@ __device__ __forceinline__ void rows_gradient(Args a, unsigned block, unsigned c
   if (row >= count) return;
   float* to = a.parts + (static_cast<int64_t>(split) * a.rows + row) * D;
 #pragma unroll
-  for (int ob = 0; ob < OB; ++ob) store_block(to, dx[ob], 1.f, 32 * ob, D, true, g);
+  for (int ob = 0; ob < OB; ++ob) store_block(to, dx[ob], 1.f, 32 * ob, a.d, true, g);
 }
 
 // dX_i = dloss_i scale (the chunks' sums - W_target).
@@ -347,7 +347,7 @@ template <typename T, int D>
 __device__ __forceinline__ void fold_rows(const Args& a, unsigned block, int groups) {
   const Folder<D> at(groups);
   const int row = block * at.rows + at.row, c = 4 * at.t;
-  const bool live = row < a.live[0];
+  const bool live = row < a.live[0] && c < a.d;
   f32x4 sum = at.sum(a.parts + static_cast<int64_t>(row) * D, a.rows * D, a.splits, groups, live);
   if (!live || at.group != 0) return;
   const T* w = static_cast<const T*>(a.w) + static_cast<int64_t>(a.c_target[row]) * a.d + c;
@@ -451,7 +451,7 @@ __device__ __forceinline__ void items_gradient(Args a, unsigned block, unsigned 
   if (a.item_splits > 1) {
     float* to = a.item_parts + (static_cast<int64_t>(split) * a.items + item) * D;
 #pragma unroll
-    for (int ob = 0; ob < OB; ++ob) store_block(to, dw[ob], 1.f, 32 * ob, D, true, g);
+    for (int ob = 0; ob < OB; ++ob) store_block(to, dw[ob], 1.f, 32 * ob, a.d, true, g);
   } else {
     T* to = static_cast<T*>(a.dw) + static_cast<int64_t>(item) * a.d;
 #pragma unroll
@@ -463,7 +463,7 @@ template <typename T, int D>
 __device__ __forceinline__ void fold_items(const Args& a, unsigned block, int groups) {
   const Folder<D> at(groups);
   const int64_t item = static_cast<int64_t>(block) * at.rows + at.row;
-  const bool live = item < a.items;
+  const bool live = item < a.items && 4 * at.t < a.d;
   const f32x4 sum = at.sum(a.item_parts + item * D, static_cast<int64_t>(a.items) * D, a.item_splits, groups, live);
   if (live && at.group == 0) store_four(static_cast<T*>(a.dw) + item * a.d, sum, 4 * at.t, a.d, a.quads);
 }

@@ -145,7 +145,7 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_kernel(Args a) 
   if (splits > 1) {
     const int64_t at = (static_cast<int64_t>(split) * pairs + pair) * (static_cast<int64_t>(a.where.max_q) * group) + r;
 #pragma unroll
-    for (int ob = 0; ob < OB; ++ob) store_block(a.part_o + at * DH, o[ob], 1.f, 32 * ob, DH, true, g);
+    for (int ob = 0; ob < OB; ++ob) store_block(a.part_o + at * DH, o[ob], 1.f, 32 * ob, a.dh, true, g);
     if (g == 0) a.part_ml[at * 2] = m, a.part_ml[at * 2 + 1] = l;
     return;
   }
@@ -166,7 +166,7 @@ __global__ __launch_bounds__(256) void sequence_attention_merge_kernel(Args a, i
   const int kv = blockIdx.x, b = blockIdx.y, pairs = a.deal.pairs.d, pair = b * a.hk + kv, group = a.group.d, splits = a.splits.d;
   const int r = blockIdx.z * at.rows + at.row;
   const Span qs = spans_of(a.where, b).q;
-  const bool live = r < qs.slot * group;
+  const bool live = r < qs.slot * group && 4 * at.t < a.dh;
   const int64_t each = static_cast<int64_t>(a.where.max_q) * group, step = pairs * each, state = pair * each + r;
   float m = -INFINITY, l = 0.f;
   f32x4 o = {0, 0, 0, 0};

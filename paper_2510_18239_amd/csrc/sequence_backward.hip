@@ -150,7 +150,7 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
   if (splits > 1) {
     float* to = a.part_q + ((static_cast<int64_t>(split) * a.where.q_rows + qs.start + query) * a.hq + head) * DH;
 #pragma unroll
-    for (int ob = 0; ob < OB; ++ob) store_block(to, dq[ob], 1.f, 32 * ob, DH, true, g);
+    for (int ob = 0; ob < OB; ++ob) store_block(to, dq[ob], 1.f, 32 * ob, a.dh, true, g);
     return;
   }
   T* out = static_cast<T*>(a.dq) + (qs.start + query) * a.dq_stride + head * a.dh;
@@ -275,7 +275,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void sequence_attentio
     const int64_t plane = static_cast<int64_t>(a.where.k_rows) * a.hk * DH;
     float* to = a.part_kv + 2 * split * plane + ((ks.start + key) * a.hk + kv) * DH;
 #pragma unroll
-    for (int ob = 0; ob < OB; ++ob) store_block(to, dk[ob], 1.f, 32 * ob, DH, true, g), store_block(to + plane, dv[ob], 1.f, 32 * ob, DH, true, g);
+    for (int ob = 0; ob < OB; ++ob) store_block(to, dk[ob], 1.f, 32 * ob, a.dh, true, g), store_block(to + plane, dv[ob], 1.f, 32 * ob, a.dh, true, g);
     return;
   }
   T* dk_row = static_cast<T*>(a.dk) + (ks.start + key) * a.dk_stride + kv * a.dh;
@@ -298,7 +298,7 @@ __global__ __launch_bounds__(256) void sequence_attention_fold_kernel(Args a, un
   const int b = blockIdx.y, i = tile * at.rows + at.row, splits = of_q ? a.q_splits.d : a.k_splits.d;
   const Spans spans = spans_of(a.where, b);
   const Span span = what == 0 ? spans.q : spans.k;
-  const bool live = i < span.slot;
+  const bool live = i < span.slot && 4 * at.t < a.dh;
   const int64_t rows = what == 0 ? a.where.q_rows : a.where.k_rows, row = span.start + i, plane = rows * heads * DH;
   const float* p = (what == 0 ? a.part_q : a.part_kv) + (what == 2 ? plane : 0) + (row * heads + head) * DH;
   f32x4 sum = at.sum(p, what == 0 ? plane : 2 * plane, splits, groups, live);

@@ -90,7 +90,7 @@ __device__ __forceinline__ void seldom() { asm volatile(""); }
 __device__ __forceinline__ constexpr int block_row(int i, int g) { return 8 * (i >> 2) + 4 * g + (i & 3); }
 
 // Tiles and chunks' sums are as wide as a power of two; products may be done for fewer columns, a multiple of 16.  (Columns of chunks' sums
-// past those are never written: the folds read them along and leave them out.)
+// past those are neither written nor read.)
 constexpr int tile_width(int c) { return c <= 32 ? 32 : c <= 64 ? 64 : c <= 128 ? 128 : 256; }
 
 template <typename T, int DH, int ROWS>
