@@ -346,6 +346,26 @@ def test_targets_that_are_not_aligned(rows):
     assert same(*(binding.lime_catalogue_loss_backward(g, x, w, t, loss[0][1]) for t in at))
 
 
+@pytest.mark.parametrize("rows,items,d", [(130, 700, 64), (600, 260, 256)])
+def test_one_gradient_of_the_loss(rows, items, d):
+    (x, _), (w, _) = make((rows, d), "bf16", 0), make((items, d), "bf16", 1)
+    t = ints(np.random.default_rng(2).integers(-9, items, rows))
+    g = torch.ones(rows, device="cuda")
+    _, lse = binding.lime_catalogue_loss(x, w, t)
+    want = binding.lime_catalogue_loss_backward(g, x, w, t, lse)
+    lib = binding.lib()
+    need = lib.lime_catalogue_loss_workspace_bytes(rows, items, d, 1, 1)
+    room = torch.empty(need, dtype=torch.uint8, device="cuda")
+    for which in (0, 1):
+        got = torch.full_like(want[which], 7.0)
+        out = [None, None]
+        out[which] = got.data_ptr()
+        status = lib.lime_catalogue_loss_backward(g.data_ptr(), x.data_ptr(), w.data_ptr(), t.data_ptr(), lse.data_ptr(), *out, rows, items, d, 1.0, 1,
+                                                  room.data_ptr(), need, torch.cuda.current_stream().cuda_stream)
+        assert status == 0, binding.last_error()
+        assert torch.equal(got, want[which])
+
+
 def test_rows_of_the_loss_that_are_not_finite_stay_alone():
     (x, _), (w, _) = make((50, 64), "bf16", 0), make((300, 64), "bf16", 1)
     t, g = ints(np.arange(50)), torch.ones(50, device="cuda")
