@@ -5,8 +5,8 @@
 // A few lanes hold a head, each the same pieces of both halves, so that a pair is in one lane and a sum takes log2(lanes) exchanges.
 // The angles of a row are the same for all its heads: a workgroup works them out once, in turns and in fp64 (at position 10^6 an
 // fp32 angle would be off by 0.06 radians), and keeps the cosines and sines in LDS.  Bound by memory: every element is read and
-// written once.  (65536 rows of eight heads of 64, bf16: forward 28 us, which is the copy's 4.8 TB/s; backward 47 us, 4.3 TB/s, and 4 for
-// the fold of the weights' gradients.)
+// written once.  (65536 rows of eight heads of 64, bf16: forward 24 us in a loop, 5.6 TB/s with what stays in the last cache, where a
+// large copy takes 4.8; backward 47 us, 4.3 TB/s, and 4 for the fold of the weights' gradients.)
 #include <math.h>
 
 #include <algorithm>
@@ -17,7 +17,12 @@
 namespace lime {
 namespace {
 
-constexpr int kRows = 8, kBackRows = 32;  // the most rows of a workgroup's turn, forward and backward
+// The most rows of a workgroup's turn, forward and backward.  Forward, the second where the first would leave half of the lanes without a
+// head: 131072 rows of eight heads of 32 39 us with turns of 8, 28 of 16, 27 of 32; 65536 of eight of 64 27.5, 24, 25; 160704 of two of
+// 20 43, 30, 33.  (Fewer rows than a thousand workgroups have need the workgroups more: 10007 rows of four of 48, fp32, both
+// directions 22.7 and 23.7.)
+constexpr int kRows = 8, kMoreRows = 16, kBackRows = 32;
+constexpr int64_t kManyRows = 16384;
 constexpr int kMaxGroups = 1024; // workgroups of a backward pass: each leaves one partial sum of the weights' gradients
 constexpr int kMaxHalf = kMaxRotaryHead / 2;
 
@@ -206,8 +211,9 @@ int64_t groups_of(int64_t rows) { return std::min<int64_t>(kMaxGroups, (rows + b
 
 template <typename T, int VEC, int PARTS>
 hipError_t launch(const Args& a, bool backward, hipStream_t s) {
-  const int64_t groups = backward ? groups_of(a.rows) : (a.rows + kRows - 1) / kRows;
+  const int64_t groups = backward ? groups_of(a.rows) : (a.rows + a.turn - 1) / a.turn;
   if (backward) hipLaunchKernelGGL((norm_rotary_kernel<T, VEC, PARTS, true, kBackRows>), dim3(static_cast<unsigned>(groups)), dim3(256), 0, s, a);
+  else if (a.turn > kRows) hipLaunchKernelGGL((norm_rotary_kernel<T, VEC, PARTS, false, kMoreRows>), dim3(static_cast<unsigned>(groups)), dim3(256), 0, s, a);
   else hipLaunchKernelGGL((norm_rotary_kernel<T, VEC, PARTS, false, kRows>), dim3(static_cast<unsigned>(groups)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
@@ -233,6 +239,7 @@ hipError_t run(const NormRotary& x, void* workspace, bool backward, hipStream_t 
   const int pieces = vectors ? half / kVec : half;
   a.lanes = 1;
   while (a.lanes < pieces && a.lanes < 64) a.lanes *= 2;
+  if (!backward && a.rows > kManyRows && std::max(a.heads[0], a.heads[1]) * kRows <= 256 / a.lanes) a.turn = kMoreRows;
   hipError_t err = vectors ? launch<T, kVec, 1>(a, backward, s) : launch<T, 1, 2>(a, backward, s);
   if (err != hipSuccess || !backward || (!x.dgamma[0] && !x.dgamma[1])) return err;
   hipLaunchKernelGGL(norm_rotary_fold_kernel<T>, dim3(static_cast<unsigned>((2 * x.dh + 3) / 4)), dim3(256), 0, s, a.partial, static_cast<int>(groups_of(x.rows)), x.dh,

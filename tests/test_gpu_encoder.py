@@ -50,7 +50,7 @@ def strided(x, before, after):
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("rows,hq,hk,dh,before,turned", [
     (1, 1, 1, 2, 0, True), (1, 4, 2, 64, 0, True), (7, 3, 1, 48, 8, True), (33, 8, 1, 128, 16, True), (9, 2, 2, 20, 0, True), (9, 2, 2, 20, 3, True),
-    (5, 1, 0, 256, 0, True), (17, 5, 3, 254, 1, True), (12, 6, 2, 80, 0, False), (2049, 4, 4, 32, 0, True), (8195, 2, 1, 16, 0, True),
+    (5, 1, 0, 256, 0, True), (17, 5, 3, 254, 1, True), (12, 6, 2, 80, 0, False), (2049, 4, 4, 32, 0, True), (8195, 2, 1, 16, 0, True), (16395, 3, 1, 24, 0, True), (16385, 1, 1, 48, 8, True),
 ])
 def test_norm_rotary(dtype, rows, hq, hk, dh, before, turned):
     u, eps, base = U[dtype], 1e-6, 10000.0
