@@ -4,7 +4,9 @@
 // Rows without a target have no loss and no gradients, and nothing of them is read into any: the other rows are listed first and, where
 // they are streamed and there are any to leave out, copied together (gather), so that padding costs no products.
 // The forward pass and dX hold rows of X in registers and stream the items' tiles, with the catalogue cut into chunks whose sums
-// are folded in ascending order; dW holds items and streams rows.  The target's own term of dX is added in fp32 at the fold.
+// are folded in ascending order; dW holds items and streams rows.  The other items' p and e are rounded to the storage type, as operands
+// of the last products (half a step each, of terms that are summed in fp32); the target's e = p - 1, which may be small beside p, is formed in
+// fp32 once a row and keeps its bits: for dX it stays out of the product and is added at the fold.
 // Bound by the matrix units: 8192 rows over 131072 items, d = 256, bf16: forward 500 us, 1.1 PFLOP/s, both gradients 1820 us with the
 // logits' products done again on either side, 1.2 PFLOP/s, where a library product of 16384^3 reaches 1.36.  (Logits kept for the
 // gradients would be 2 GB written and read twice, as long as the product that they save.)
@@ -286,7 +288,8 @@ __global__ __launch_bounds__(256) void catalogue_loss_kernel(Args a) {
   }
 }
 
-// sum_v p_iv W_v over a chunk of the catalogue, 32 rows a wave.
+// sum_v p_iv W_v, v other than target(i), over a chunk of the catalogue, 32 rows a wave.  (The target's p among them, rounded, would leave
+// nothing of p - 1 where a row has learnt its target: from p = 0.998 on, dX was off by as much as itself.)
 template <typename T, int C, int STEP>
 __device__ __forceinline__ void rows_gradient(Args a, unsigned block, unsigned char* smem) {
   constexpr int D = tile_width(C);
@@ -308,6 +311,7 @@ __device__ __forceinline__ void rows_gradient(Args a, unsigned block, unsigned c
   Fragment<T> x[NK];
   load_row<T, C>(static_cast<const T*>(a.x) + static_cast<int64_t>(row < count ? a.live[1 + row] : 0) * a.d, width, a.x_pieces, row < count, g, x);
   const float c = a.scale * kLog2e, lse2 = row < count ? a.c_lse2[row] : 0.f;
+  const int own = row < count ? a.c_target[row] - v0 - 4 * g : -8;  // the target, from the chunk's first item of this lane half
   f32x16 dx[OB];
 #pragma unroll
   for (int ob = 0; ob < OB; ++ob) dx[ob] = zero_block();
@@ -322,11 +326,13 @@ __device__ __forceinline__ void rows_gradient(Args a, unsigned block, unsigned c
       for (int kk = 0; kk < NK; ++kk) p = mma16(read.row(wt, 32 * vb, kk), x[kk], p);
 #pragma unroll
       for (int e = 0; e < 16; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(p[e], c, -lse2));
-      if (v0 + (i + 1) * STEP > v1) {
-        seldom();  // (zero rows past the chunk: p may be infinite there)
+      const int first = i * STEP + 32 * vb;
+      // some row's target is in this block, or zero rows past the chunk, where p may be infinite
+      if (__any(static_cast<unsigned>(own - first) < 32u) || first + 32 > v1 - v0) {
+        seldom();
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (v0 + i * STEP + 32 * vb + block_row(e, g) >= v1) p[e] = 0.f;
+          if (own - first == block_row(e, 0) || v1 - v0 - first - 4 * g <= block_row(e, 0)) p[e] = 0.f;
       }
 #pragma unroll
       for (int f = 0; f < 2; ++f) {
@@ -342,7 +348,7 @@ __device__ __forceinline__ void rows_gradient(Args a, unsigned block, unsigned c
   for (int ob = 0; ob < OB; ++ob) store_block(to, dx[ob], 1.f, 32 * ob, a.d, true, g);
 }
 
-// dX_i = dloss_i scale (the chunks' sums - W_target).
+// dX_i = dloss_i scale the chunks' sums + e_target W_target.
 template <typename T, int D>
 __device__ __forceinline__ void fold_rows(const Args& a, unsigned block, int groups) {
   const Folder<D> at(groups);
@@ -351,10 +357,10 @@ __device__ __forceinline__ void fold_rows(const Args& a, unsigned block, int gro
   f32x4 sum = at.sum(a.parts + static_cast<int64_t>(row) * D, a.rows * D, a.splits, groups, live);
   if (!live || at.group != 0) return;
   const T* w = static_cast<const T*>(a.w) + static_cast<int64_t>(a.c_target[row]) * a.d + c;
-  const float f = a.c_g[row];
+  const float f = a.c_g[row], e = a.c_e[row];
 #pragma unroll
   for (int j = 0; j < 4; ++j)
-    if (c + j < a.d) sum[j] = f * (sum[j] - to_float(w[j]));
+    if (c + j < a.d) sum[j] = fmaf(f, sum[j], e * to_float(w[j]));
   store_four(static_cast<T*>(a.dx) + static_cast<int64_t>(a.live[1 + row]) * a.d, sum, c, a.d, a.quads);
 }
 
