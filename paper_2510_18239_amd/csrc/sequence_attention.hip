@@ -208,7 +208,8 @@ __global__ __launch_bounds__(256) void sequence_attention_merge_kernel(Args a, i
 constexpr int keys_of(bool bf16, int dh) { return !bf16 ? 32 : dh <= 32 ? 128 : 64; }
 
 struct Plan {
-  int waves, keys, tiles, splits, chunk, dh;  // dh: padded
+  int waves, keys, splits, chunk, dh;  // dh: padded
+  int64_t tiles;  // (the workspace's size is answered also where they pass what a launch takes)
   size_t o_bytes, bytes;
 };
 
@@ -227,7 +228,7 @@ Plan plan_of(const SequenceAttention& a) {
   p.dh = tile_width(dh);
   p.waves = rows <= 32 ? 1 : 4;
   p.keys = p.waves > 1 ? keys_of(dtype == 1, p.dh) : 32;
-  p.tiles = static_cast<int>((rows + 32 * p.waves - 1) / (32 * p.waves));
+  p.tiles = (rows + 32 * p.waves - 1) / (32 * p.waves);
   const int64_t groups = B * hk * p.tiles;
   const int64_t want = (p.waves == 1 ? 8 : 2) * static_cast<int64_t>(compute_units());
   const int64_t least = p.waves == 1 ? std::max<int64_t>(dtype == 1 ? 128 : 32, (max_k + 255) / 256) : dtype == 1 ? 256 : 128;
@@ -274,7 +275,7 @@ bool sequence_attention_fits(const SequenceAttention& a) {  // 2^32 work items a
   const int64_t rows = static_cast<int64_t>(a.max_q) * (a.hq / a.hk), pairs = static_cast<int64_t>(a.B) * a.hk;
   if (rows >= (int64_t{1} << 31) - 128 || pairs >= (int64_t{1} << 24)) return false;
   const Plan p = plan_of(a);
-  const int64_t deep = static_cast<int64_t>(p.tiles) * p.splits;
+  const int64_t deep = p.tiles * p.splits;
   return deep < 65536 && pairs * deep < (int64_t{1} << 26) / p.waves;  // (where keys are cut, pairs times rows are less than 2^17)
 }
 
@@ -291,7 +292,7 @@ hipError_t sequence_attention(const SequenceAttention& x, void* workspace, hipSt
   a.where = Packing(x), a.deal = Deal(x, p.splits == 1 || (p.waves == 1 && x.B * x.hk % 8 == 0)), a.o = x.O, a.lse = x.lse;
   a.part_o = static_cast<float*>(workspace), a.part_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.o_bytes);
   a.B = x.B, a.hq = x.hq, a.hk = x.hk, a.dh = x.dh;
-  a.group = Divisor(x.hq / x.hk), a.splits = Divisor(p.splits), a.tiles = p.tiles, a.chunk = p.chunk;
+  a.group = Divisor(x.hq / x.hk), a.splits = Divisor(p.splits), a.tiles = static_cast<int>(p.tiles), a.chunk = p.chunk;
   a.c = std::max(fabsf(x.scale) * kLog2e, 1e-37f), a.negate = x.scale < 0.f, a.causal = x.causal != 0;
   a.pieces = multiple(x.Q, 16) && multiple(x.K, 16) && multiple(x.V, 16) && x.dh * e % 16 == 0 && x.q_stride * e % 16 == 0 &&
              x.k_stride * e % 16 == 0 && x.v_stride * e % 16 == 0;

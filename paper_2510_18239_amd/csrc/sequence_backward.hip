@@ -311,7 +311,8 @@ __global__ __launch_bounds__(256) void sequence_attention_fold_kernel(Args a, un
 }
 
 struct Plan {
-  int dh, q_tiles, k_tiles, q_splits, q_chunk, k_splits, k_chunk;
+  int dh, q_splits, q_chunk, k_splits, k_chunk;
+  int64_t q_tiles, k_tiles;  // (the workspace's size is answered also where they pass what a launch takes)
   size_t stats, part_q, part_kv, bytes;
 };
 
@@ -324,7 +325,7 @@ Plan plan_of(const SequenceAttention& a) {
   const int64_t want = 2 * static_cast<int64_t>(compute_units()), step = a.dtype == 1 ? 64 : 32;
   Plan p{};
   p.dh = tile_width(a.dh);
-  p.q_tiles = static_cast<int>((max_q * group + 127) / 128), p.k_tiles = static_cast<int>((max_k + 127) / 128);
+  p.q_tiles = (max_q * group + 127) / 128, p.k_tiles = (max_k + 127) / 128;
   auto cut = [&](int64_t tiles, int64_t length, int64_t least, int64_t want, int& splits, int& chunk) {
     const int64_t most = std::max<int64_t>(1, (length + least - 1) / least), n = std::min(most, std::max<int64_t>(1, (want + pairs * tiles - 1) / (pairs * tiles)));
     const int64_t c = ((length + n - 1) / n + step - 1) / step * step;
@@ -350,8 +351,8 @@ hipError_t run(Args a, const Plan& p, int users, hipStream_t s) {
     static PerDevice granted;
     const auto kernel = sequence_attention_dq_kernel<T, C, 4, STEP>;
     if (hipError_t e = allow_lds(granted, reinterpret_cast<const void*>(kernel), lds); e != hipSuccess) return e;
-    a.tiles = p.q_tiles;
-    hipLaunchKernelGGL(kernel, dim3(a.hk, users, p.q_tiles * p.q_splits), dim3(256), lds, s, a);
+    a.tiles = static_cast<int>(p.q_tiles);
+    hipLaunchKernelGGL(kernel, dim3(a.hk, users, a.tiles * p.q_splits), dim3(256), lds, s, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
   if (max_k > 0) {
@@ -359,7 +360,7 @@ hipError_t run(Args a, const Plan& p, int users, hipStream_t s) {
     static PerDevice granted;
     const auto kernel = sequence_attention_dkv_kernel<T, C, STEP>;
     if (hipError_t e = allow_lds(granted, reinterpret_cast<const void*>(kernel), lds); e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3(a.hk, users, p.k_tiles * p.k_splits), dim3(256), lds, s, a);
+    hipLaunchKernelGGL(kernel, dim3(a.hk, users, static_cast<unsigned>(p.k_tiles * p.k_splits)), dim3(256), lds, s, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
   const bool q_folds = p.q_splits > 1 && max_q > 0, k_folds = p.k_splits > 1 && max_k > 0;
@@ -379,7 +380,7 @@ bool sequence_attention_backward_fits(const SequenceAttention& a) {  // 2^32 wor
   const int64_t rows = static_cast<int64_t>(a.max_q) * (a.hq / a.hk), pairs = static_cast<int64_t>(a.B) * a.hk;
   if (rows >= (int64_t{1} << 31) - 128 || pairs >= (int64_t{1} << 24)) return false;
   const Plan p = plan_of(a);
-  const int64_t q_deep = static_cast<int64_t>(p.q_tiles) * p.q_splits, k_deep = static_cast<int64_t>(p.k_tiles) * p.k_splits;
+  const int64_t q_deep = p.q_tiles * p.q_splits, k_deep = p.k_tiles * p.k_splits;
   // (of a side that is cut, users times heads times rows are less than 2^18: a side with more has workgroups enough)
   return q_deep < 65536 && k_deep < 65536 && pairs * q_deep < (int64_t{1} << 24) && pairs * k_deep < (int64_t{1} << 24);
 }
