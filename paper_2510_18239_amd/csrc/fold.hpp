@@ -26,12 +26,17 @@ struct Folder {
   }
   // The sum of the chunks' states at p, `step` floats apart, in every lane of group 0.  All threads of the workgroup call it.
   __device__ f32x4 sum(const float* p, int64_t step, int splits, int groups, bool live) const {
+    return sum_of([&](int s) { return *reinterpret_cast<const f32x4*>(p + s * step + 4 * t); }, splits, groups, live);
+  }
+  // The sum of chunk(s) over the chunks s, in the same way.
+  template <typename F>
+  __device__ f32x4 sum_of(F chunk, int splits, int groups, bool live) const {
     __shared__ f32x4 met[256];
     f32x4 a = {0, 0, 0, 0};
     if (live) {
 #pragma unroll 4
       for (int s = group; s < splits; s += groups) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(p + s * step + 4 * t);
+        const f32x4 x = chunk(s);
 #pragma unroll
         for (int j = 0; j < 4; ++j) a[j] += x[j];
       }

@@ -3,9 +3,16 @@
 //   dQ_i = scale sum_j e_ij K_j,   dK_j = scale sum_i e_ij Q_i,   dV_j = sum_i p_ij G_i   (i over all heads that share the key head).
 // Two kernels, each with one side's rows and sums in registers while the other side's tiles stream past, so that every sum has one
 // owner and one order (no atomics): the first holds queries (rows as in the forward pass) and also leaves -D and lse, by head, for
-// the second, which holds keys.  Seven products of the tiles where a kernel that kept both sides' sums would do five: the sums of
-// the other side would have to meet in memory.  Where the workgroups of a side are too few for the chip, the side that streams past is
-// cut into chunks whose sums a third kernel folds (fold.hpp).  p and e are rounded to the storage type, as operands of the last products.
+// the second, which holds keys.  A kernel that kept both sides' sums would do five products of the tiles where these do seven or eight: the
+// sums of the other side would have to meet in memory.  Where the workgroups of a side are too few for the chip, the side that streams past is
+// cut into chunks whose sums a third kernel folds (fold.hpp).  p and e are rounded to the storage type, as operands of the last products
+// (half a step of each, of terms that are summed in fp32).
+// D is held in fp32, and an O of bf16 gives it only to 2^-8 of <|G|, |O|>, which may be more than all of e: of a row whose softmax is
+// nearly decided, that sees few keys, or whose values have a large part in common.  (One key of 300 to 2000 with p up to 0.9999, or values
+// of 8 + noise: dQ off by as much as itself to ten times that.)  So the first kernel takes e from that D, sums e on the way, gap_i = sum_j e_ij,
+// which is what D lacks, and takes gap_i sum_j p_ij K_j off its sums at the end, one more product of the key tile that it has; the
+// second gets the whole D.  (16 causal histories of 4096 events, four heads on two, d/h = 64, forward and gradients: 660 us without, 708 with.
+// D from products of its own beforehand would be two more.)
 // Bound as the forward pass is: 16 causal histories of 4096 events, four heads on two, d/h = 64 500 us, 960 TFLOP/s of the seven
 // products; d/h = 128 1030 us, 930.
 #include <algorithm>
@@ -24,7 +31,7 @@ struct Args {
   const float* lse;
   float *lse2, *less;  // [hq][q_rows]: lse log2 e, -D
   void *dq, *dk, *dv;
-  float *part_q, *part_kv;  // chunks > 1: [q_splits][q_rows][hq][padded dh], [k_splits][2][k_rows][hk][padded dh]
+  float *part_q, *part_gap, *part_kv;  // chunks > 1: [q_splits][1 or 2][q_rows][hq][padded dh], [q_splits][q_rows][hq], [k_splits][2][k_rows][hk][padded dh]
   Divisor group, q_splits, k_splits;
   int hq, hk, dh, tiles;
   int q_chunk, k_chunk;  // chunks of keys (in keys), and of the steps over queries
@@ -32,8 +39,17 @@ struct Args {
   bool pieces, causal, quads;
 };
 
+// Whether O has been rounded to fewer bits than D is held in.
+template <typename T>
+constexpr bool kRounded = sizeof(T) == 2;
+// Whether the kernel that holds queries has to save registers for a second wave a SIMD: block by block, and with D taken off <G, V> where its
+// sums would start from a block of -D.  (16 causal histories of 4096 events, forward and gradients: d/h = 128 1518 us without, 1435 so;
+// 96 1152 and 1062; at 64 there are two waves in any case, 708 and 730.)
+template <typename T, int C>
+constexpr bool kTight = sizeof(T) == 2 && C > 80;
+
 template <typename T, int C, int WAVES, int KEYS>
-__global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args a) {
+__global__ __launch_bounds__(WAVES * 64, (kTight<T, C> ? 2 : 1)) void sequence_attention_dq_kernel(Args a) {
   constexpr int DH = tile_width(C);
   using Stage = Stages<T, DH, KEYS, 2>;  // keys, values
   using Loader = TileLoader<T, DH, KEYS, WAVES>;
@@ -67,12 +83,7 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
     kl.issue(km, i * KEYS, k_end - k_begin, Stage::tile(smem, i, 0), tid);
     vl.issue(vm, i * KEYS, k_end - k_begin, Stage::tile(smem, i, 1), tid);
   };
-  // Few keys: all their tiles fit, and D comes from its other form, sum_j p_ij <G_i, V_j>.  <G_i, O_i> carries the rounding of O to
-  // the storage type, which is as large as the difference e_ij where a row sees two keys and fades with the square root of their
-  // number (two keys, bf16: gradients 5e-3 off from the rounded O, 2.6e-3 this way; past 128 keys the two are alike).
-  const bool resident = sizeof(T) == 2 && most <= 2 * KEYS;  // (and in one chunk, none is shorter)
   if (steps > 0) ask(0);
-  if (resident && steps > 1) ask(1);
 
   const int64_t row = (qs.start + query) * a.hq + head;
   Fragment<T> q[NK], go[NK];
@@ -80,23 +91,7 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
   load_row<T, C>(static_cast<const T*>(a.go) + row * a.dh, width, a.pieces, live, g, go);
   const float c = a.scale * kLog2e, lse2 = live ? a.lse[row] * kLog2e : 0.f;
   float delta = 0.f;
-  if (resident) {
-    wait_lds_loads<0>();
-    lds_barrier();
-    for (int kb = 0; kb < KB * steps; ++kb) {
-      const unsigned rows = kb % KB * 32 * Reader::kRowBytes, kt = Stage::operand(smem, kb / KB, 0) + rows, vt = Stage::operand(smem, kb / KB, 1) + rows;
-      f32x16 s = zero_block(), e = zero_block();
-#pragma unroll
-      for (int kk = 0; kk < NK; ++kk) {
-        s = mma16(read.row(kt, 0, kk), q[kk], s);
-        e = mma16(read.row(vt, 0, kk), go[kk], e);
-      }
-#pragma unroll
-      for (int x = 0; x < 16; ++x)
-        if (32 * kb + block_row(x, g) < limit) delta = fmaf(__builtin_amdgcn_exp2f(fmaf(s[x], c, -lse2)), e[x], delta);
-    }
-    delta = pair_sum(delta);
-  } else {
+  {
     Fragment<T> o[NK];
     load_row<T, C>(static_cast<const T*>(a.o) + row * a.dh, width, a.pieces, live, g, o);
 #pragma unroll
@@ -105,53 +100,77 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_dq_kernel(Args 
       for (int t = 0; t < 8; ++t) delta = fmaf(element(go[kk], t), element(o[kk], t), delta);
     delta = pair_sum(delta);
   }
-  if (live && g == 0 && split == 0) {
-    const int64_t at = head * static_cast<int64_t>(a.where.q_rows) + qs.start + query;
-    a.lse2[at] = lse2, a.less[at] = -delta;
-  }
-  f32x16 dq[OB], less;  // less: -D, where the sums <G_i, V_j> - D_i start from
+  f32x16 dq[OB], mean[kRounded<T> ? OB : 1], less;  // less: -D, where the sums <G_i, V_j> - D_i start from
+  float gap = 0.f;  // of the lane half's keys
 #pragma unroll
-  for (int ob = 0; ob < OB; ++ob) dq[ob] = zero_block();
+  for (int ob = 0; ob < OB; ++ob) {
+    dq[ob] = zero_block();
+    if constexpr (kRounded<T>) mean[ob] = zero_block();
+  }
 #pragma unroll
   for (int x = 0; x < 16; ++x) less[x] = -delta;
 
   for (int i = 0; i < steps; ++i) {
     Stage::template arrive<WAVES>(smem, tid);
-    if (i + 1 < steps && !resident) ask(i + 1);
+    if (i + 1 < steps) ask(i + 1);
     const int key0 = k_begin + i * KEYS;
     if (key0 >= wave_most) continue;
     const unsigned kt = Stage::operand(smem, i, 0), vt = Stage::operand(smem, i, 1);
     const bool partial = key0 + KEYS > wave_least;
-#pragma unroll
+#pragma unroll(kTight<T, C> ? 1 : KB)
     for (int kb = 0; kb < KB; ++kb) {
-      f32x16 s = zero_block(), e = less;
+      f32x16 s = zero_block(), e = kTight<T, C> ? zero_block() : less;
 #pragma unroll
       for (int kk = 0; kk < NK; ++kk) {
         s = mma16(read.row(kt, 32 * kb, kk), q[kk], s);
         e = mma16(read.row(vt, 32 * kb, kk), go[kk], e);
       }
 #pragma unroll
-      for (int x = 0; x < 16; ++x) e[x] *= __builtin_amdgcn_exp2f(fmaf(s[x], c, -lse2));
+      for (int x = 0; x < 16; ++x) s[x] = __builtin_amdgcn_exp2f(fmaf(s[x], c, -lse2)), e[x] = (kTight<T, C> ? e[x] - delta : e[x]) * s[x];
       if (partial) {
         seldom();
 #pragma unroll
         for (int x = 0; x < 16; ++x)
-          if (key0 + 32 * kb + block_row(x, g) >= limit) e[x] = 0.f;
+          if (key0 + 32 * kb + block_row(x, g) >= limit) s[x] = 0.f, e[x] = 0.f;
+      }
+      if constexpr (kRounded<T>) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) gap += e[x];
       }
 #pragma unroll
       for (int f = 0; f < 2; ++f) {
-        const Fragment<T> ef = half_fragment<T>(e, f);
+        const Fragment<T> ef = half_fragment<T>(e, f), pf = half_fragment<T>(s, f);
 #pragma unroll
-        for (int ob = 0; ob < OB; ++ob) dq[ob] = mma16(read.column(kt, 32 * kb + 16 * f, 32 * ob), ef, dq[ob]);
+        for (int ob = 0; ob < OB; ++ob) {
+          const Fragment<T> k = read.column(kt, 32 * kb + 16 * f, 32 * ob);
+          dq[ob] = mma16(k, ef, dq[ob]);
+          if constexpr (kRounded<T>) mean[ob] = mma16(k, pf, mean[ob]);
+        }
       }
     }
   }
   if (r >= slot_rows) return;
+  gap = pair_sum(gap);
+  if (live && g == 0 && split == 0) {
+    const int64_t at = head * static_cast<int64_t>(a.where.q_rows) + qs.start + query;
+    a.lse2[at] = lse2, a.less[at] = splits > 1 ? -delta : -delta - gap;  // (of chunks, the fold adds the gaps)
+  }
   if (splits > 1) {
-    float* to = a.part_q + ((static_cast<int64_t>(split) * a.where.q_rows + qs.start + query) * a.hq + head) * DH;
+    const int64_t plane = static_cast<int64_t>(a.where.q_rows) * a.hq * DH;
+    float* to = a.part_q + (kRounded<T> ? 2 : 1) * split * plane + row * DH;
 #pragma unroll
-    for (int ob = 0; ob < OB; ++ob) store_block(to, dq[ob], 1.f, 32 * ob, a.dh, true, g);
+    for (int ob = 0; ob < OB; ++ob) {
+      store_block(to, dq[ob], 1.f, 32 * ob, a.dh, true, g);
+      if constexpr (kRounded<T>) store_block(to + plane, mean[ob], 1.f, 32 * ob, a.dh, true, g);
+    }
+    if (kRounded<T> && g == 0) a.part_gap[static_cast<int64_t>(split) * a.where.q_rows * a.hq + row] = gap;
     return;
+  }
+  if constexpr (kRounded<T>) {
+#pragma unroll
+    for (int ob = 0; ob < OB; ++ob)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) dq[ob][x] = fmaf(-gap, mean[ob][x], dq[ob][x]);
   }
   T* out = static_cast<T*>(a.dq) + (qs.start + query) * a.dq_stride + head * a.dh;
 #pragma unroll
@@ -301,7 +320,14 @@ __global__ __launch_bounds__(256) void sequence_attention_fold_kernel(Args a, un
   const bool live = i < span.slot && 4 * at.t < a.dh;
   const int64_t rows = what == 0 ? a.where.q_rows : a.where.k_rows, row = span.start + i, plane = rows * heads * DH;
   const float* p = (what == 0 ? a.part_q : a.part_kv) + (what == 2 ? plane : 0) + (row * heads + head) * DH;
-  f32x4 sum = at.sum(p, what == 0 ? plane : 2 * plane, splits, groups, live);
+  f32x4 sum = at.sum(p, what == 0 && !kRounded<T> ? plane : 2 * plane, splits, groups, live);
+  if (kRounded<T> && what == 0) {  // (the same for the whole workgroup)
+    const f32x4 mean = at.sum(p + plane, 2 * plane, splits, groups, live);
+    const float gap = at.sum_of([&](int s) { return f32x4{a.part_gap[(s * rows + row) * heads + head], 0, 0, 0}; }, splits, groups, live)[0];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum[j] = fmaf(-gap, mean[j], sum[j]);
+    if (i < span.used && at.t == 0 && at.group == 0) a.less[head * rows + row] -= gap;
+  }
   if (!live || at.group != 0) return;
   const float factor = what == 2 ? 1.f : a.scale;
 #pragma unroll
@@ -313,7 +339,7 @@ __global__ __launch_bounds__(256) void sequence_attention_fold_kernel(Args a, un
 struct Plan {
   int dh, q_splits, q_chunk, k_splits, k_chunk;
   int64_t q_tiles, k_tiles;  // (the workspace's size is answered also where they pass what a launch takes)
-  size_t stats, part_q, part_kv, bytes;
+  size_t stats, part_q, part_gap, part_kv, bytes;
 };
 
 // Two workgroups of four waves a compute unit are wanted; no chunk is shorter than 256 keys (bf16; 128: fp32), or four steps over queries.
@@ -336,9 +362,10 @@ Plan plan_of(const SequenceAttention& a) {
   cut(p.k_tiles, steps * step, 4 * step, ragged(a) && a.dtype == 1 ? 2 * want : want, p.k_splits, p.k_chunk);
   p.k_chunk = static_cast<int>((p.k_chunk + step - 1) / step);
   p.stats = align_up(static_cast<size_t>(a.q_rows) * a.hq * sizeof(float));
-  p.part_q = p.q_splits > 1 ? align_up(static_cast<size_t>(p.q_splits) * a.q_rows * a.hq * p.dh * sizeof(float)) : 0;
+  const size_t states = p.q_splits > 1 ? static_cast<size_t>(p.q_splits) * a.q_rows * a.hq * sizeof(float) : 0;
+  p.part_q = align_up(states * p.dh * (a.dtype == 1 ? 2 : 1)), p.part_gap = a.dtype == 1 ? align_up(states) : 0;
   p.part_kv = p.k_splits > 1 ? align_up(static_cast<size_t>(p.k_splits) * 2 * a.k_rows * a.hk * p.dh * sizeof(float)) : 0;
-  p.bytes = std::max<size_t>(256, 2 * p.stats + p.part_q + p.part_kv);
+  p.bytes = std::max<size_t>(256, 2 * p.stats + p.part_q + p.part_gap + p.part_kv);
   return p;
 }
 
@@ -355,6 +382,16 @@ hipError_t run(Args a, const Plan& p, int users, hipStream_t s) {
     hipLaunchKernelGGL(kernel, dim3(a.hk, users, a.tiles * p.q_splits), dim3(256), lds, s, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
+  const bool q_folds = p.q_splits > 1 && max_q > 0, k_folds = p.k_splits > 1 && max_k > 0;
+  const int q_groups = fold_groups(p.q_splits, DH / 4), k_groups = fold_groups(p.k_splits, DH / 4);
+  auto fold = [&](bool q, bool k) {
+    auto blocks = [](int rows, int groups, int heads) { const int per = 256 / (DH / 4) / groups; return static_cast<unsigned>((rows + per - 1) / per * heads); };
+    const unsigned q_blocks = q ? blocks(max_q, q_groups, a.hq) : 0, k_blocks = k ? blocks(max_k, k_groups, 2 * a.hk) : 0;
+    hipLaunchKernelGGL((sequence_attention_fold_kernel<T, DH>), dim3(q_blocks + k_blocks, users), dim3(256), 0, s, a, q_blocks, q_groups, k_groups);
+    return hipGetLastError();
+  };
+  if (kRounded<T> && q_folds)  // D is whole
+    if (hipError_t e = fold(true, false); e != hipSuccess) return e;
   if (max_k > 0) {
     constexpr int lds = Stages<T, DH, STEP, 2, 2>::kBytes;
     static PerDevice granted;
@@ -363,13 +400,8 @@ hipError_t run(Args a, const Plan& p, int users, hipStream_t s) {
     hipLaunchKernelGGL(kernel, dim3(a.hk, users, static_cast<unsigned>(p.k_tiles * p.k_splits)), dim3(256), lds, s, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
-  const bool q_folds = p.q_splits > 1 && max_q > 0, k_folds = p.k_splits > 1 && max_k > 0;
-  if (!q_folds && !k_folds) return hipSuccess;
-  const int q_groups = fold_groups(p.q_splits, DH / 4), k_groups = fold_groups(p.k_splits, DH / 4);
-  auto blocks = [](int rows, int groups, int heads) { const int per = 256 / (DH / 4) / groups; return static_cast<unsigned>((rows + per - 1) / per * heads); };
-  const unsigned q_blocks = q_folds ? blocks(max_q, q_groups, a.hq) : 0, k_blocks = k_folds ? blocks(max_k, k_groups, 2 * a.hk) : 0;
-  hipLaunchKernelGGL((sequence_attention_fold_kernel<T, DH>), dim3(q_blocks + k_blocks, users), dim3(256), 0, s, a, q_blocks, q_groups, k_groups);
-  return hipGetLastError();
+  const bool q_left = q_folds && !kRounded<T>;
+  return q_left || k_folds ? fold(q_left, k_folds) : hipSuccess;
 }
 
 bool multiple(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
@@ -399,6 +431,7 @@ hipError_t sequence_attention_backward(const SequenceAttention& x, void* workspa
   a.lse2 = reinterpret_cast<float*>(at), at += p.stats;
   a.less = reinterpret_cast<float*>(at), at += p.stats;
   a.part_q = reinterpret_cast<float*>(at), at += p.part_q;
+  a.part_gap = reinterpret_cast<float*>(at), at += p.part_gap;
   a.part_kv = reinterpret_cast<float*>(at);
   a.group = Divisor(x.hq / x.hk), a.q_splits = Divisor(p.q_splits), a.q_chunk = p.q_chunk, a.k_splits = Divisor(p.k_splits), a.k_chunk = p.k_chunk;
   a.hq = x.hq, a.hk = x.hk, a.dh = x.dh;
