@@ -386,8 +386,8 @@ int32_t lime_scores(const lime_scoring_model* model, const void* E, const int32_
  * Strides are at least a row's own elements and below 2^24 bytes.  Pointers, strides and head rows that are multiples of 16 bytes
  * are read 16 bytes a lane, anything else element by element (slower; sums may be in another order).  Workspaces are 256-byte aligned.
  * Outputs overlap neither inputs nor each other, unless it is said that they may.  Refused with LIME_UNSUPPORTED: more than 65535 users
- * or heads, users whose rows make more than 65535 tiles of 128 (32 where a key head's queries are no more), 2^25 rows or more than 2^30
- * items of the loss, 2^27 rows or more of the rotation.
+ * or heads, users whose rows make more than 65535 tiles of 128 (32 where a key head's queries are no more) or who may have more than 2^31 - 256
+ * keys, 2^25 rows or more than 2^30 items of the loss, 2^27 rows or more of the rotation.
  */
 typedef struct lime_sequences {
   const int32_t *q_offsets, *k_offsets; /* [B + 1] */

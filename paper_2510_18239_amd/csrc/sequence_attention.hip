@@ -61,7 +61,8 @@ __global__ __launch_bounds__(WAVES * 64) void sequence_attention_kernel(Args a) 
   const int w0 = r0 + 32 * wave, wave_most = w0 < used_rows ? last_limit(min(w0 + 32, used_rows)) : 0;
   const int wave_least = w0 + 32 <= used_rows ? keys_seen(a.group.divide(w0), n_q, n_k, a.causal) : 0;
   const int most = r0 < used_rows ? last_limit(min(r0 + ROWS, used_rows)) : 0;
-  const int k_begin = split * a.chunk, k_end = splits > 1 ? min(most, k_begin + a.chunk) : most;
+  // (no sum a chunk past the last key: there may be nearly 2^31)
+  const int k_begin = split * a.chunk, k_end = splits > 1 ? k_begin + min(most - k_begin, a.chunk) : most;
   const int steps = k_end > k_begin ? (k_end - k_begin + KEYS - 1) / KEYS : 0;
 
   const T* kp = static_cast<const T*>(a.k) + (ks.start + k_begin) * a.k_stride + kv * a.dh;
@@ -271,9 +272,11 @@ bool multiple(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) %
 
 }  // namespace
 
+constexpr int64_t kMostKeys = (int64_t{1} << 31) - 256;  // a step past them is still a number of 32 bits
+
 bool sequence_attention_fits(const SequenceAttention& a) {  // 2^32 work items a launch, 65535 workgroups along the grid's third axis
   const int64_t rows = static_cast<int64_t>(a.max_q) * (a.hq / a.hk), pairs = static_cast<int64_t>(a.B) * a.hk;
-  if (rows >= (int64_t{1} << 31) - 128 || pairs >= (int64_t{1} << 24)) return false;
+  if (rows >= (int64_t{1} << 31) - 128 || pairs >= (int64_t{1} << 24) || a.max_k > kMostKeys) return false;
   const Plan p = plan_of(a);
   const int64_t deep = p.tiles * p.splits;
   return deep < 65536 && pairs * deep < (int64_t{1} << 26) / p.waves;  // (where keys are cut, pairs times rows are less than 2^17)

@@ -76,6 +76,6 @@ hipError_t at_head_width(int dh, F f) {
 }
 
 // How many keys query i of a user sees: all, or those up to its own place counted from the end.
-__device__ __forceinline__ int keys_seen(int i, int n_q, int n_k, bool causal) { return causal ? min(n_k, max(0, i + 1 + n_k - n_q)) : n_k; }
+__device__ __forceinline__ int keys_seen(int i, int n_q, int n_k, bool causal) { return causal ? min(n_k, max(0, n_k - n_q + (i + 1))) : n_k; }
 
 }  // namespace lime

@@ -26,3 +26,10 @@ def test_sizes_of_shapes_whose_tiles_pass_32_bits(backward):
                 assert need >= 2 * w.q_rows * hq * 4  # two words a query and head
             else:  # fewer than 2^17 rows' states in all chunks together
                 assert 256 <= need <= (1 << 17) * (128 + 2) * 4 + 512
+
+
+@pytest.mark.parametrize("k_rows,max_k,status", [((1 << 31) - 1, (1 << 31) - 1, 2), ((1 << 31) - 255, (1 << 31) - 1, 2), ((1 << 31) - 1, (1 << 31) - 256, 3), (1 << 30, (1 << 31) - 1, 3)])
+def test_most_keys(k_rows, max_k, status):
+    """Slots that may end within a step of 2^31 are refused; a longest slot past the tensor counts as the tensor's rows."""
+    w = binding.Sequences(FAKE, FAKE, None, None, 1, k_rows, 1, 1, max_k)
+    assert binding.lib().lime_sequence_attention(ctypes.byref(w), FAKE, 8, FAKE, 8, FAKE, 8, FAKE, FAKE, 1, 1, 8, 1.0, 1, 1, FAKE, 0, None) == status
