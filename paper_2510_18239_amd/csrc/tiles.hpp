@@ -240,7 +240,8 @@ struct TileLoader {
         unsigned at_row;  // (added here, not by the compiler: it would keep all the sums in registers across the kernel's loop)
         asm volatile("s_mov_b32 m0, %1\n\tv_add_u32_e32 %0, %2, %3\n\tbuffer_load_dwordx4 %0, %4, 0 offen lds"
                      : "=&v"(at_row)
-                     : "s"(lds + WAVES * 1024 * i), "s"(i / kOffsets * kOffsets * kRowsALoad * m.stride), "v"(offset[i % kOffsets]), "s"(resource));
+                     : "s"(lds + WAVES * 1024 * i), "s"(i / kOffsets * kOffsets * kRowsALoad * m.stride), "v"(offset[i % kOffsets]), "s"(resource)
+                     : "m0");
       }
     } else {
       const unsigned columns = m.width / sizeof(T);
@@ -263,7 +264,7 @@ __device__ __forceinline__ void words_to_lds(const void* from, int count, void* 
   resource[2] = __builtin_amdgcn_readfirstlane(count * 4u);
   resource[3] = 0x00020000u;
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
-               : : "s"(__builtin_amdgcn_readfirstlane(lds_offset_of(to))), "v"(lane * 4u), "s"(resource));
+               : : "s"(__builtin_amdgcn_readfirstlane(lds_offset_of(to))), "v"(lane * 4u), "s"(resource) : "m0");
 }
 
 // The 16-deep fragments of one row of `width` bytes, straight from memory: lane half g's slots hold columns 16 kk + 8g .. + 7.
