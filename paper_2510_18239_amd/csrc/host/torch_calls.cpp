@@ -20,8 +20,11 @@
 
 #include <algorithm>
 #include <array>
+#include <functional>
 #include <initializer_list>
 #include <map>
+#include <mutex>
+#include <tuple>
 #include <utility>
 #include <vector>
 
@@ -193,13 +196,21 @@ class Unlocked {
   PyThreadState* state_;
 };
 
-// One entry point of the library.  Its arguments are values: a tensor's pointer is taken at the call, under the lock, where
-// a tensor that has none (vmap's and other wrappers) may raise.
+// The lock of a stream (one of 64, by its handle).  A call is several launches that hand on data in the workspace, which the calls on a
+// stream share: two threads that call on one stream must not mix theirs.  Taken without the interpreter lock, given back before that is.
+std::mutex& order_of(void* stream) {
+  static auto* locks = new std::array<std::mutex, 64>();  // (never destroyed: threads may still call)
+  return (*locks)[std::hash<void*>()(stream) / 64 % locks->size()];
+}
+
+// One entry point of the library; its last argument is the stream.  Its arguments are values: a tensor's pointer is taken at the call, under
+// the lock, where a tensor that has none (vmap's and other wrappers) may raise.
 template <typename... P, typename... A>
 void call(int32_t (*entry_point)(P...), A... args) {
   int32_t status;
   {
     Unlocked unlocked;
+    const std::lock_guard<std::mutex> one_at_a_time(order_of(std::get<sizeof...(A) - 1>(std::tuple<A...>(args...))));
     status = entry_point(args...);
   }
   if (status != LIME_OK) lime_failed(status, lime_last_error());
