@@ -18,9 +18,10 @@ namespace lime {
 namespace {
 
 // The most rows of a workgroup's turn, forward and backward.  Forward, the second where the first would leave half of the lanes without a
-// head: 131072 rows of eight heads of 32 39 us with turns of 8, 28 of 16, 27 of 32; 65536 of eight of 64 27.5, 24, 25; 160704 of two of
-// 20 43, 30, 33.  (Fewer rows than a thousand workgroups have need the workgroups more: 10007 rows of four of 48, fp32, both
-// directions 22.7 and 23.7.)
+// head of one side, and has no more heads of either than lanes for them: bf16, 131072 rows of 4 + 4 heads of 32 39 us with turns of 8, 28 of
+// 16, 27 of 32; 65536 of 4 + 4 of 64 27.5, 24, 25; of 8 + 1 of 64 27.5 and 25.3; 160704 of 1 + 1 of 20 43, 30, 33.  (Where eight rows fill the
+// lanes of both sides: 65536 of 8 + 8 of 64 50.5 us with turns of 8, 53.2 of 16; of 4 + 4 of 128 52.2 and 50.3; of 4 + 4 of 64 in fp32 43.9 and
+// 47.1.  Fewer rows than a thousand workgroups have need the workgroups more: 10007 rows of 3 + 1 of 48, fp32, both directions 22.7 and 23.7.)
 constexpr int kRows = 8, kMoreRows = 16, kBackRows = 32;
 constexpr int64_t kManyRows = 16384;
 constexpr int kMaxGroups = 1024; // workgroups of a backward pass: each leaves one partial sum of the weights' gradients
@@ -239,7 +240,8 @@ hipError_t run(const NormRotary& x, void* workspace, bool backward, hipStream_t 
   const int pieces = vectors ? half / kVec : half;
   a.lanes = 1;
   while (a.lanes < pieces && a.lanes < 64) a.lanes *= 2;
-  if (!backward && a.rows > kManyRows && std::max(a.heads[0], a.heads[1]) * kRows <= 256 / a.lanes) a.turn = kMoreRows;
+  const int units = 256 / a.lanes, most = std::max(a.heads[0], a.heads[1]), least = a.heads[1] > 0 ? std::min(a.heads[0], a.heads[1]) : a.heads[0];
+  if (!backward && a.rows > kManyRows && most * kRows <= units && 2 * least * kRows <= units) a.turn = kMoreRows;
   hipError_t err = vectors ? launch<T, kVec, 1>(a, backward, s) : launch<T, 1, 2>(a, backward, s);
   if (err != hipSuccess || !backward || (!x.dgamma[0] && !x.dgamma[1])) return err;
   hipLaunchKernelGGL(norm_rotary_fold_kernel<T>, dim3(static_cast<unsigned>((2 * x.dh + 3) / 4)), dim3(256), 0, s, a.partial, static_cast<int>(groups_of(x.rows)), x.dh,
