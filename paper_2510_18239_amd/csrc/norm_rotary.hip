@@ -128,7 +128,21 @@ __global__ __launch_bounds__(256, BACKWARD ? 4 : 1) void norm_rotary_kernel(Args
 #pragma unroll
           for (int i = 0; i < VEC; ++i) square = fmaf(lo[p][i], lo[p][i], fmaf(hi[p][i], hi[p][i], square));
         }
-        const float inverse = 1.f / sqrtf(lanes_sum(square, a.lanes) / a.dh + a.eps);
+        const float total = lanes_sum(square, a.lanes) / a.dh + a.eps;
+        float inverse = 1.f / sqrtf(total);
+        if (__any(!(total >= 0x1p-60f && total < INFINITY))) {
+          seldom();  // squares past the range of fp32, at either end: again, of entries that are 2^70 times smaller or larger
+          const float f = total < 1.f ? 0x1p70f : 0x1p-70f;
+          square = 0.f;
+#pragma unroll
+          for (int p = 0; p < PARTS; ++p) {
+            if ((t + p * a.lanes) * VEC >= half) continue;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) square = fmaf(lo[p][i] * f, lo[p][i] * f, fmaf(hi[p][i] * f, hi[p][i] * f, square));
+          }
+          const float again = f / sqrtf(lanes_sum(square, a.lanes) / a.dh + a.eps * f * f);
+          if (!(total >= 0x1p-60f && total < INFINITY)) inverse = again;
+        }
         float mean = 0.f;
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
