@@ -366,7 +366,8 @@ int32_t lime_scores(const lime_scoring_model* model, const void* E, const int32_
  *   n_q > n_k the first queries see nothing.  causal = 0: every query sees all keys of its user.
  *   A row that sees no key gets zeros.  Rows of a slot not in use are never read and get zeros in O; rows outside all slots are left
  *   as they were.  Entries that are not finite stay with their user (a key that a query does not see may still turn the rows of
- *   its user's neighbouring queries to NaN if its value row is not finite).
+ *   its user's neighbouring queries to NaN if its value row is not finite).  In fp32 an infinite entry counts as NaN, here and in the
+ *   loss: products are formed from parts of their operands.
  *   lse [q_rows][hq] fp32, nullable: log sum_j exp(scale <Q_i, K_j>), -infinity for rows that see nothing or are not in use.
  *   Few queries over many keys (serving) have the keys cut into chunks whose states are folded by a second kernel.
  * lime_sequence_attention_backward - dQ, dK, dV from dO and the forward pass's inputs and outputs O, lse (same sizes, same

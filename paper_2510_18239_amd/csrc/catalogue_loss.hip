@@ -7,7 +7,7 @@
 // are folded in ascending order; dW holds items and streams rows.  The other items' p and e are rounded to the storage type, as operands
 // of the last products (half a step each, of terms that are summed in fp32); the target's e = p - 1, which may be small beside p, is formed in
 // fp32 once a row and keeps its bits: for dX it stays out of the product and is added at the fold.
-// Bound by the matrix units: 8192 rows over 131072 items, d = 256, bf16: forward 500 us, 1.1 PFLOP/s, both gradients 1820 us with the
+// Bound by the matrix units: 8192 rows over 131072 items, d = 256, bf16: forward 500 us, 1.1 PFLOP/s, both gradients 1840 us with the
 // logits' products done again on either side, 1.2 PFLOP/s, where a library product of 16384^3 reaches 1.36.  (Logits kept for the
 // gradients would be 2 GB written and read twice, as long as the product that they save.)
 #include <algorithm>
@@ -513,7 +513,8 @@ struct Plan {
 Plan plan_of(int64_t rows, int items, int d, int dtype, bool backward) {
   Plan p{};
   const int step = dtype == 1 ? 64 : 32, D = tile_width(d);
-  // (up to 64 columns leave a unit the registers of four workgroups: 20000 rows over 20000 items, d = 64, 369 us with two, 325 with four)
+  // (up to 64 columns a unit has room for four workgroups, but for three of the gradients' at 33 to 64, whose registers the fourth waits for:
+  // 20000 rows over 20000 items, d = 64, both directions, 369 us with two, 325 with four)
   const int64_t want = (D <= 64 ? 4 : 2) * static_cast<int64_t>(compute_units());
   const double step_us = D / 128. * (dtype == 1 ? 1 : 1.5);
   p.rows = cut((rows + 127) / 128, items, step, want, rows * (backward ? D : 2), step_us);
@@ -595,7 +596,8 @@ hipError_t backward(const Args& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// f(width) for the narrowest width of products that holds d columns
+// f(width) for the narrowest width of products that there is for d columns.  (224 was made for d = 200; d from 129 to 192 have none of their
+// own and do up to 56 % more products than they need.)
 template <typename F>
 hipError_t at_width(int d, F f) {
   if (d <= 32) return f(std::integral_constant<int, 32>{});

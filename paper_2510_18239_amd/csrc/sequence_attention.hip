@@ -4,6 +4,8 @@
 // holds one query row and the softmax's statistics are the lane's own and its partner's; p = exp2(S c - m) rounded to the storage
 // type is, as it stands, the operand of O^T += V^T P^T.  The rows of a workgroup are pairs (query, head of the group) that share a
 // key head, in memory order: a tile of keys and values is read once for a whole group, in a prompt as for a single query.
+// (Half a step of each p, of terms that fp32 sums hold, over the sum of the unrounded ones: against 64 bits O is off by 0.0023 of itself
+// where fp32 p would leave the 0.0017 of its own rounding.)
 // Bound by the vector units (a step's exponentials, scalings, maxima and sums are 930 of their cycles beside 512 of the matrix units at
 // d/h = 64) and, with few rows, by the latency of a step: 16 causal histories of 4096 events, four heads on two, d/h = 64 160 us,
 // 860 TFLOP/s; d/h = 128 275 us, 1 PFLOP/s; four users' single events over up to 131072 keys, d/h = 128: 4.1 TB/s.
@@ -216,11 +218,12 @@ struct Plan {
 
 // Rows that one wave holds take a workgroup of one wave.  Where the tiles of rows are too few to fill the chip, the keys are cut
 // into chunks as well.  A lone wave needs about 1600 cycles for a step of 32 keys, most of them waiting for itself, and 4600 to start
-// and to end: so eight waves a compute unit are wanted, of four steps at least (fp32, where a step takes 4 us at d/h = 128: of one), but
-// no more than 256 chunks of a row, which have to be folded again.  (32 users, up to 4096 keys: 14.6 us in chunks of 128 keys, 15.8 of
+// and to end: so eight waves a compute unit are wanted, but no more chunks than four steps (fp32, where a step takes 4 us at d/h = 128: one)
+// go into the keys, and no more than 256 of a row, which have to be folded again.  (32 users, up to 4096 keys: 14.6 us in chunks of 128 keys, 15.8 of
 // 256; four users of up to 131072: 53 us in 512 chunks, 49 in 256; fp32, two users, up to 249 keys: 27.9 us in chunks of 128, 12.5 of
 // 32.  More tiles in flight take the LDS of the other waves: three 16.0, four 15.7 and 51.9.)  Of workgroups of four waves, two a
-// compute unit, of 256 keys at least (fp32: 128).  (8 users' up to 64 new events over up to 8192 keys: 17.6 us, 19.0 with one workgroup
+// compute unit, but no more chunks than 256 keys (fp32: 128) go into the keys.  Chunks are of whole steps and as long as each other but for the
+// last, so that 257 keys in two are 192 and 65.  (8 users' up to 64 new events over up to 8192 keys: 17.6 us, 19.0 with one workgroup
 // a unit or 512 keys, 23 with four and 128; five users' up to 501 events in fp32: 21.2 us, 24.5 with 256.)
 Plan plan_of(const SequenceAttention& a) {
   const int64_t B = a.B, hk = a.hk, max_k = std::max(a.max_k, 1), rows = std::max<int64_t>(a.max_q, 1) * (a.hq / a.hk);

@@ -13,8 +13,10 @@
 // which is what D lacks, and takes gap_i sum_j p_ij K_j off its sums at the end, one more product of the key tile that it has; the
 // second gets the whole D.  (16 causal histories of 4096 events, four heads on two, d/h = 64, forward and gradients: 660 us without, 708 with.
 // D from products of its own beforehand would be two more.)
-// Bound as the forward pass is: 16 causal histories of 4096 events, four heads on two, d/h = 64 500 us, 960 TFLOP/s of the seven
-// products; d/h = 128 1030 us, 930.
+// Bound by the two units waiting for each other: matrix cores busy 45 and 38 % of the time in the two kernels, the vector units about half
+// (of the second, at d/h = 64: 512 cycles of products and some 620 of exponentials, products and rounding a block of 32 queries, which takes
+// 1350; two waves a SIMD are not enough to cover for each other).  16 causal histories of 4096 events, four heads on two, d/h = 64
+// 560 us, 980 TFLOP/s of the eight products, 615 of the five; d/h = 128 1170 us, 940 and 590.
 #include <algorithm>
 
 #include "fold.hpp"
@@ -177,8 +179,8 @@ __global__ __launch_bounds__(WAVES * 64, (kTight<T, C> ? 2 : 1)) void sequence_a
   for (int ob = 0; ob < OB; ++ob) store_block(out, dq[ob], a.scale, 32 * ob, a.dh, a.quads, g);
 }
 
-// (bf16, d/h = 128: kept to 256 registers, with eight of a wave's loaded again for every 32 queries, for a second wave a SIMD: 16 causal
-// histories of 4096 events 1150 us with one, 1030 with two.)
+// (bf16, d/h = 128: kept to 256 registers, with eight of a wave's loaded again for every 32 queries, for a second wave a SIMD: 120 us less
+// of the 1150 that 16 causal histories of 4096 events took with one, both kernels.)
 template <typename T, int C, int STEP>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void sequence_attention_dkv_kernel(Args a) {
   constexpr int DH = tile_width(C);
@@ -342,7 +344,11 @@ struct Plan {
   size_t stats, part_q, part_gap, part_kv, bytes;
 };
 
-// Two workgroups of four waves a compute unit are wanted; no chunk is shorter than 256 keys (bf16; 128: fp32), or four steps over queries.
+// Two workgroups of four waves a compute unit are wanted, but no more chunks than 256 keys (bf16; 128: fp32) or four steps over queries
+// go into the length; chunks are of whole steps and as long as each other but for the last.
+// In bf16 the fold of dQ is a launch of its own, and up to 512 keys of heads up to 64 are not cut: three users of up to 500 events, d/h = 32, 38.4 us in
+// chunks of 256 and 36.2 whole; eight of 512, 64, 54.8 and 50.9; but three of up to 500, 128, 76.8 and 79.3, and with chunks of 512 two of 1000, 128,
+// 72.2 and 82.1, 64 new events over 8192, d/h = 64, 44.3 and 46.8.
 // Of ragged users twice as many for the kernel that holds keys: its workgroups are few, and the longest user's first keys see all of that
 // user's queries of all heads of the group.  (Four users of 79 to 3983 events, eight heads on two, d/h = 80: 775 us with two a unit, 553
 // with four; 52 of up to 551, eight heads on one, 122 and 103; 16 of 3129 each 314 and 342; in fp32, where a unit holds one, 162 and 177.)
@@ -357,7 +363,8 @@ Plan plan_of(const SequenceAttention& a) {
     const int64_t c = ((length + n - 1) / n + step - 1) / step * step;
     chunk = static_cast<int>(std::min<int64_t>(c, (int64_t{1} << 31) - 1)), splits = static_cast<int>((length + c - 1) / c);
   };
-  cut(p.q_tiles, max_k, 4 * step, want, p.q_splits, p.q_chunk);
+  const bool whole = a.dtype == 1 && p.dh <= 64 && max_k <= 8 * step;  // not worth the fold
+  cut(p.q_tiles, max_k, whole ? max_k : 4 * step, want, p.q_splits, p.q_chunk);
   const int64_t steps = (max_q + step - 1) / step * group;
   cut(p.k_tiles, steps * step, 4 * step, ragged(a) && a.dtype == 1 ? 2 * want : want, p.k_splits, p.k_chunk);
   p.k_chunk = static_cast<int>((p.k_chunk + step - 1) / step);

@@ -11,7 +11,8 @@
 // parts that reach into them (the three left out are below 2^-24 of it): six bf16 instructions of 32 cycles where
 // v_mfma_f32_32x32x2_f32 takes eight of 64.  An fp32 tile is cut once, by all waves of the workgroup together, into three tiles of
 // bf16 (Stages).  (When every wave cut the fragments it read: 1003 rows over 20011 items with both gradients 161 us, now 152.)
-// An operand that is not finite gives NaN; one below 2^-110 loses its last parts to the instruction's range.
+// An operand that is not finite gives NaN (an infinite one too: its parts are it and what is left of it less itself); one below 2^-110
+// loses its last parts to the instruction's range.
 #pragma once
 
 #include <type_traits>
