@@ -6,7 +6,7 @@
 // The forward pass and dX hold rows of X in registers and stream the items' tiles, with the catalogue cut into chunks whose sums
 // are folded in ascending order; dW holds items and streams rows.  The other items' p and e are rounded to the storage type, as operands
 // of the last products (half a step each, of terms that are summed in fp32); the target's e = p - 1, which may be small beside p, is formed in
-// fp32 once a row and keeps its bits: for dX it stays out of the product and is added at the fold.
+// fp32 once a row, from the stored lse (whose own rounding is what is left of its error): for dX it stays out of the product and is added at the fold.
 // Bound by the matrix units: 8192 rows over 131072 items, d = 256, bf16: forward 500 us, 1.1 PFLOP/s, both gradients 1840 us with the
 // logits' products done again on either side, 1.2 PFLOP/s, where a library product of 16384^3 reaches 1.36.  (Logits kept for the
 // gradients would be 2 GB written and read twice, as long as the product that they save.)
@@ -35,7 +35,8 @@ struct Args {
   // workspace
   int32_t* live;      // [1 + rows]: how many rows have a target, and which they are
   void* packed;       // [rows][d] the rows with a target, written where some have none
-  float *c_lse2, *c_g, *c_e;  // [rows] of the listed rows: lse log2 e; dloss scale; e of the target
+  float *c_logit;             // forward, [rows] of the listed rows: <X_i, W_target>
+  float *c_lse2, *c_g, *c_e;  // backward, [rows] of the listed rows: lse log2 e; dloss scale; e of the target
   int32_t *c_target, *c_place;  // [rows] the target, and its place among the tiles of items
   Divisor item_tiles;
   float* parts;       // forward [splits][rows][2], dX [splits][rows][padded d]
@@ -52,6 +53,30 @@ __device__ __forceinline__ int place_of(const Args& a, int item) {
   return (item - at * static_cast<int>(a.item_tiles.d)) * 128 + at;
 }
 
+// <X_i, W_target> of 32 rows, a lane pair each, with the very bits that the forward pass's stream of tiles gives it: the same instructions in the
+// same order, of -X for a negative scale (a sum of opposite terms need not be the opposite), and the diagonal of the block.  Of a learnt target
+// lse and the logit nearly cancel.  (300 rows over 1000 items, d = 256, p of the target from 0.6 to 0.9999, median errors with a sum in another
+// order, and with this: loss 9e-5 of itself and 1e-5, in fp32 dX 2.4e-4 and 2.7e-5.)
+template <typename T>
+__device__ __forceinline__ float target_logits(const Args& a, int64_t row, int target, bool live, int lane) {
+  const int n = lane & 31, g = lane >> 5;
+  const T *x = static_cast<const T*>(a.x) + row * a.d, *w = static_cast<const T*>(a.w) + static_cast<int64_t>(target) * a.d;
+  f32x16 s = zero_block();
+#pragma unroll 4
+  for (int c = 0; c < a.d; c += 16) {
+    Fragment<T> xf[1], wf[1];
+    load_row<T, 16>(x + c, (a.d - c) * sizeof(T), a.x_pieces, live, g, xf);
+    load_row<T, 16>(w + c, (a.d - c) * sizeof(T), a.w_pieces, live, g, wf);
+    if (a.scale < 0.f) negate(xf[0]);
+    s = mma16(wf[0], xf[0], s);
+  }
+  float own = 0.f;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) own = block_row(e, g) == n ? s[e] : own;
+  own = pair_sum(own);
+  return a.scale < 0.f ? -own : own;
+}
+
 constexpr int kGatherRows = 64, kGatherWaves = 16;  // rows a workgroup of the gather takes at a time
 
 // Lists the rows with a target.  Every workgroup counts all targets by itself (they are few next to the products), so that no
@@ -59,11 +84,10 @@ constexpr int kGatherRows = 64, kGatherWaves = 16;  // rows a workgroup of the g
 template <typename T, bool BACKWARD>
 __global__ __launch_bounds__(64 * kGatherWaves) void gather_kernel(Args a, int64_t each) {
   __shared__ int sums[kGatherWaves][2];
-  __shared__ int place[kGatherRows];
+  __shared__ int place[kGatherRows], aim[kGatherRows];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t begin = blockIdx.x * each, end = min(begin + each, a.rows);
   auto named = [&](int target) { return static_cast<unsigned>(target) < static_cast<unsigned>(a.items); };
-  auto has = [&](int64_t i) { return named(a.targets[i]); };
   int before = 0, all = 0;
   auto count = [&](int64_t i, int target) {
     const int x = named(target);
@@ -87,14 +111,15 @@ __global__ __launch_bounds__(64 * kGatherWaves) void gather_kernel(Args a, int64
   for (int64_t at = begin; at < end; at += kGatherRows) {
     if (wave == 0) {  // 64 rows' places
       const int64_t i = at + lane;
-      const bool x = i < end && has(i);
+      const int target = i < end ? a.targets[i] : -1;
+      const bool x = named(target);
       const unsigned long long votes = __ballot(x);
       const int to = before + __popcll(votes & ((1ull << lane) - 1));
       before += __popcll(votes);
-      place[lane] = x ? to : -1;
+      place[lane] = x ? to : -1, aim[lane] = target;
       if (x) {
         a.live[1 + to] = static_cast<int>(i);
-        if constexpr (BACKWARD) a.c_lse2[to] = a.lse[i] * kLog2e, a.c_g[to] = a.dloss[i] * a.scale, a.c_target[to] = a.targets[i], a.c_place[to] = place_of(a, a.targets[i]);
+        if constexpr (BACKWARD) a.c_lse2[to] = a.lse[i] * kLog2e, a.c_g[to] = a.dloss[i] * a.scale, a.c_target[to] = target, a.c_place[to] = place_of(a, target);
       } else if (i < end) {
         if constexpr (!BACKWARD) a.loss[i] = 0.f, a.lse[i] = 0.f;
       }
@@ -102,18 +127,18 @@ __global__ __launch_bounds__(64 * kGatherWaves) void gather_kernel(Args a, int64
     if constexpr (!BACKWARD) continue;
     __syncthreads();
     const int here = static_cast<int>(min<int64_t>(kGatherRows, end - at));
+    if (wave < 2) {  // e of the rows' own targets, dloss scale (p - 1): 32 rows a wave
+      const int r = 32 * wave + (lane & 31), to = r < here ? place[r] : -1;
+      const int64_t i = at + min(r, here - 1);
+      const float lse = to >= 0 ? a.lse[i] : 0.f, weight = to >= 0 ? a.dloss[i] : 0.f;
+      const float s = target_logits<T>(a, i, to >= 0 ? aim[r] : 0, to >= 0, lane);
+      if (to >= 0 && lane < 32) a.c_e[to] = (__builtin_amdgcn_exp2f(fmaf(s, a.scale, -lse) * kLog2e) - 1.f) * weight * a.scale;
+    }
 #pragma unroll 4
     for (int r = wave; r < here; r += kGatherWaves) {  // a wave a row
+      if (whole) continue;
       const T* from = static_cast<const T*>(a.x) + (at + r) * a.d;
       const int to = place[r];
-      if (to >= 0) {  // e of the row's own target, dloss scale (p - 1)
-        const T* w = static_cast<const T*>(a.w) + static_cast<int64_t>(a.targets[at + r]) * a.d;
-        float z = 0.f;
-        for (int c = lane; c < a.d; c += 64) z = fmaf(to_float(from[c]), to_float(w[c]), z);
-        z = wave_sum(z) * a.scale - a.lse[at + r];
-        if (lane == 0) a.c_e[to] = (__builtin_amdgcn_exp2f(z * kLog2e) - 1.f) * a.dloss[at + r] * a.scale;
-      }
-      if (whole) continue;
       T* dst = to >= 0 ? static_cast<T*>(a.packed) + static_cast<int64_t>(to) * a.d : static_cast<T*>(a.dx) + (at + r) * a.d;
       if (to < 0 && a.dx == nullptr) continue;
       if (a.x_pieces && a.quads) {  // rows of whole 16-byte pieces: at most 64 of them
@@ -136,9 +161,9 @@ __global__ __launch_bounds__(64 * kGatherWaves) void gather_kernel(Args a, int64
 }
 
 // Few rows are listed by every wave of the forward pass for itself: a look at all targets, 64 at a time, takes less than another
-// kernel.  The wave's 32 places from `first` on get the rows that stand there; returns how many rows are listed in all.
+// kernel.  The wave's 32 places from `first` on get the rows that stand there and their targets; returns how many rows are listed in all.
 constexpr int kFewRows = 4096;
-__device__ __forceinline__ int list_rows(const Args& a, int first, int lane, int32_t* places, bool zero_others) {
+__device__ __forceinline__ int list_rows(const Args& a, int first, int lane, int2* places, bool zero_others) {
   int before = 0;
   const int rows = static_cast<int>(a.rows);
   for (int base = 0; base < rows; base += 512) {
@@ -151,7 +176,7 @@ __device__ __forceinline__ int list_rows(const Args& a, int first, int lane, int
       const bool x = i < rows && static_cast<unsigned>(target[j]) < static_cast<unsigned>(a.items);
       const unsigned long long votes = __ballot(x);
       const int to = before + __popcll(votes & ((1ull << lane) - 1)) - first;
-      if (x && static_cast<unsigned>(to) < 32u) places[to] = i;
+      if (x && static_cast<unsigned>(to) < 32u) places[to] = {i, target[j]};
       if (zero_others && !x && i < rows) a.loss[i] = 0.f, a.lse[i] = 0.f;
       before += __popcll(votes);
     }
@@ -160,7 +185,7 @@ __device__ __forceinline__ int list_rows(const Args& a, int first, int lane, int
   return before;
 }
 
-// Running maximum and sum of a chunk of the catalogue for 32 rows a wave.
+// Running maximum and sum of a chunk of the catalogue for 32 rows a wave; the last workgroups, one a tile of rows, have the rows' own logits.
 template <typename T, int C, int STEP>
 __global__ __launch_bounds__(256) void catalogue_lse_kernel(Args a) {
   constexpr int D = tile_width(C);
@@ -171,26 +196,34 @@ __global__ __launch_bounds__(256) void catalogue_lse_kernel(Args a) {
   extern __shared__ __align__(1024) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
   const Reader read(lane);
-  const int split = blockIdx.x % a.splits, tile = blockIdx.x / a.splits, row = tile * 128 + 32 * wave + n;
-  const int v0 = split * a.chunk, v1 = min(a.items, v0 + a.chunk), steps = (v1 - v0 + STEP - 1) / STEP;
+  const int tiles = static_cast<int>((a.rows + 127) / 128), block = blockIdx.x;
+  const bool streams = block < tiles * a.splits;
+  const int split = streams ? block % a.splits : a.splits, tile = streams ? block / a.splits : block - tiles * a.splits, row = tile * 128 + 32 * wave + n;
+  const int v0 = streams ? split * a.chunk : 0, v1 = streams ? min(a.items, v0 + a.chunk) : 0, steps = (v1 - v0 + STEP - 1) / STEP;
   const unsigned width = a.d * sizeof(T);
   const Rows wm{static_cast<const T*>(a.w) + static_cast<int64_t>(v0) * a.d, width, width, a.w_pieces};
   Loader wl;
   wl.init(wm, tid);
-  wl.issue(wm, 0, v1 - v0, Stage::tile(smem, 0, 0), tid);
-  int count, from = 0;
+  if (streams) wl.issue(wm, 0, v1 - v0, Stage::tile(smem, 0, 0), tid);
+  int count, from = 0, target = 0;
   if (a.rows <= kFewRows) {
-    int32_t* places = reinterpret_cast<int32_t*>(smem + Stage::kTiles) + 32 * wave;  // (where the first step's tile does not arrive)
+    int2* places = reinterpret_cast<int2*>(smem + Stage::kTiles) + 32 * wave;  // (where the first step's tile does not arrive)
     count = list_rows(a, row - n, lane, places, split == 0 && tile == 0 && wave == 0);
-    if (row < count) from = places[n];
+    if (row < count) from = places[n].x, target = places[n].y;
     if (split == 0 && g == 0 && row < count) a.live[1 + row] = from;
     if (split == 0 && row == 0 && g == 0) a.live[0] = count;
   } else {
     count = a.live[0];
     if (row < count) from = a.live[1 + row];
+    if (row < count && !streams) target = a.targets[from];
   }
   if (tile * 128 >= count) {
     wait_lds_loads<0>();
+    return;
+  }
+  if (!streams) {
+    const float s = target_logits<T>(a, from, target, row < count, lane);
+    if (row < count && g == 0) a.c_logit[row] = s;
     return;
   }
   Fragment<T> x[NK];
@@ -261,12 +294,10 @@ __global__ __launch_bounds__(256) void catalogue_lse_kernel(Args a) {
   }
 }
 
-// A wave a row: the chunks' states folded, and the target's logit.
-template <typename T>
+// A wave a row: the chunks' states folded, and the target's logit taken off.
 __global__ __launch_bounds__(256) void catalogue_loss_kernel(Args a) {
   const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6), count = a.live[0];
   if (row >= count) return;
-  const int at = a.live[1 + row], target = a.targets[at];
   float m = -INFINITY, l = 0.f;
   for (int s = lane; s < a.splits; s += 64) {
     const float* p = a.parts + (static_cast<int64_t>(s) * a.rows + row) * 2;
@@ -278,13 +309,11 @@ __global__ __launch_bounds__(256) void catalogue_loss_kernel(Args a) {
   for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o, 64));
   const float base = most == -INFINITY ? 0.f : most;
   const float sum = wave_sum(l * __builtin_amdgcn_exp2f(m - base));
-  const T *x = static_cast<const T*>(a.x) + static_cast<int64_t>(at) * a.d, *w = static_cast<const T*>(a.w) + static_cast<int64_t>(target) * a.d;
-  float z = 0.f;
-  for (int c = lane; c < a.d; c += 64) z = fmaf(to_float(x[c]), to_float(w[c]), z);
-  z = wave_sum(z) * a.scale;
   if (lane == 0) {
-    const float lse = (most + __builtin_amdgcn_logf(sum)) * kLn2;
-    a.lse[at] = lse, a.loss[at] = lse - z;
+    // (off the maximum as it went into it, in base 2; lse from both with one rounding where the target has a good part of it)
+    const int at = a.live[1 + row];
+    const float s = a.c_logit[row], rest = __builtin_amdgcn_logf(sum), loss = (fmaf(-s, a.scale * kLog2e, most) + rest) * kLn2;
+    a.lse[at] = loss < 1.f ? fmaf(s, a.scale, loss) : (most + rest) * kLn2, a.loss[at] = loss;
   }
 }
 
@@ -521,16 +550,16 @@ Plan plan_of(int64_t rows, int items, int d, int dtype, bool backward) {
   p.items = cut((static_cast<int64_t>(items) + 127) / 128, rows, step, want, static_cast<int64_t>(items) * D, step_us);
   p.live = align_up((rows + 1) * sizeof(int32_t));
   p.packed = backward ? align_up(static_cast<size_t>(rows) * d * (dtype == 1 ? 2 : 4)) : 0;
-  p.listed = backward ? align_up(rows * sizeof(float)) : 0;
+  p.listed = align_up(rows * sizeof(float));
   p.parts = align_up(static_cast<size_t>(p.rows.splits) * rows * (backward ? D : 2) * sizeof(float));
   p.item_parts = backward && p.items.splits > 1 ? align_up(static_cast<size_t>(p.items.splits) * items * D * sizeof(float)) : 0;
-  p.bytes = p.live + p.packed + 5 * p.listed + p.parts + p.item_parts;
+  p.bytes = p.live + p.packed + (backward ? 5 : 1) * p.listed + p.parts + p.item_parts;
   return p;
 }
 
 bool multiple(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
-Args args_of(const CatalogueLoss& x, const Plan& p, void* workspace) {
+Args args_of(const CatalogueLoss& x, const Plan& p, bool backward, void* workspace) {
   const size_t e = x.dtype == 1 ? 2 : 4;
   Args a{};
   a.x = x.X, a.w = x.W, a.targets = x.targets, a.loss = x.loss, a.lse = x.lse, a.dloss = x.dloss, a.dx = x.dX, a.dw = x.dW;
@@ -541,11 +570,15 @@ Args args_of(const CatalogueLoss& x, const Plan& p, void* workspace) {
   char* at = static_cast<char*>(workspace);
   a.live = reinterpret_cast<int32_t*>(at), at += p.live;
   a.packed = at, at += p.packed;
-  a.c_lse2 = reinterpret_cast<float*>(at), at += p.listed;
-  a.c_g = reinterpret_cast<float*>(at), at += p.listed;
-  a.c_e = reinterpret_cast<float*>(at), at += p.listed;
-  a.c_target = reinterpret_cast<int32_t*>(at), at += p.listed;
-  a.c_place = reinterpret_cast<int32_t*>(at), at += p.listed;
+  if (backward) {
+    a.c_lse2 = reinterpret_cast<float*>(at), at += p.listed;
+    a.c_g = reinterpret_cast<float*>(at), at += p.listed;
+    a.c_e = reinterpret_cast<float*>(at), at += p.listed;
+    a.c_target = reinterpret_cast<int32_t*>(at), at += p.listed;
+    a.c_place = reinterpret_cast<int32_t*>(at), at += p.listed;
+  } else {
+    a.c_logit = reinterpret_cast<float*>(at), at += p.listed;
+  }
   a.parts = reinterpret_cast<float*>(at), at += p.parts;
   a.item_parts = reinterpret_cast<float*>(at);
   a.splits = p.rows.splits, a.chunk = p.rows.chunk, a.item_splits = p.items.splits, a.item_chunk = p.items.chunk;
@@ -573,8 +606,8 @@ hipError_t forward(const Args& a, hipStream_t s) {
   if (a.rows > kFewRows)
     if (hipError_t e = gather<T, false>(a, s); e != hipSuccess) return e;
   static PerDevice granted;
-  if (hipError_t e = launch(granted, catalogue_lse_kernel<T, C, STEP>, (a.rows + 127) / 128 * a.splits, Stages<T, D, STEP, 1>::kBytes, s, a); e != hipSuccess) return e;
-  hipLaunchKernelGGL(catalogue_loss_kernel<T>, dim3(static_cast<unsigned>((a.rows + 3) / 4)), dim3(256), 0, s, a);
+  if (hipError_t e = launch(granted, catalogue_lse_kernel<T, C, STEP>, (a.rows + 127) / 128 * (a.splits + 1), Stages<T, D, STEP, 1>::kBytes, s, a); e != hipSuccess) return e;
+  hipLaunchKernelGGL(catalogue_loss_kernel, dim3(static_cast<unsigned>((a.rows + 3) / 4)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
@@ -618,13 +651,13 @@ size_t catalogue_loss_workspace(int64_t rows, int items, int d, int dtype, bool 
 
 hipError_t catalogue_loss(const CatalogueLoss& x, void* workspace, hipStream_t s) {
   const Plan p = plan_of(x.rows, x.items, x.d, x.dtype, false);
-  const Args a = args_of(x, p, workspace);
+  const Args a = args_of(x, p, false, workspace);
   return at_width(x.d, [&](auto width) { return x.dtype == 1 ? forward<bf16_t, width.value>(a, s) : forward<float, width.value>(a, s); });
 }
 
 hipError_t catalogue_loss_backward(const CatalogueLoss& x, void* workspace, hipStream_t s) {
   const Plan p = plan_of(x.rows, x.items, x.d, x.dtype, true);
-  const Args a = args_of(x, p, workspace);
+  const Args a = args_of(x, p, true, workspace);
   return at_width(x.d, [&](auto width) { return x.dtype == 1 ? backward<bf16_t, width.value>(a, s) : backward<float, width.value>(a, s); });
 }
 

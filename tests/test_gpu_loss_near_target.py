@@ -77,3 +77,29 @@ def test_a_decided_row_is_still_pulled_to_its_target():
         # half a step for p of the other as an operand and for the result; fp32: the logits' 40 F of |z| and the logarithm's steps, over q
         allowed = 2 * q * (2 * U["bf16"]) + 2 * (F * 40 * 3 * z + 16 * F)
         assert abs(dX.double().cpu().numpy() + 2 * q).max() <= allowed
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,d,scale", [(400, 256, 0.0625), (5000, 64, 0.125), (37, 100, -0.1)])
+def test_loss_of_learnt_rows_among_large_logits(dtype, rows, d, scale):
+    """Eight items whose logits all lie near 100 in size, so that lse and a target's logit agree in most of their bits: what is left is the loss.
+    The target's logit is the one that went into lse, so that of its error only 1 - p is left, and of lse's sum the rounding of its few terms."""
+    items, r = 8, np.random.default_rng(rows)
+    W = torch.from_numpy(r.standard_normal((items, d))).to(DT[dtype])
+    common = torch.from_numpy(np.sign(scale) * 100.0 / (abs(scale) * d) * np.ones(d))
+    W = (W.double() + 1.0).to(DT[dtype])
+    w, t = W.double().numpy(), r.integers(0, items, rows)
+    gap = np.linspace(0.0, 12.0, rows)
+    apart = w[t] - w.mean(0)
+    X = torch.from_numpy(common.numpy() + apart * (gap / ((apart * w[t]).sum(1) * scale))[:, None]).to(DT[dtype])
+    x = X.double().numpy()
+    loss, lse = binding.lime_catalogue_loss(X.cuda(), W.cuda(), ints(t), scale)
+    want, wlse, e = enc.catalogue_loss(x, w, t, scale)
+    L = abs(scale) * (abs(x) @ abs(w).T).max(1)
+    rest = -e[np.arange(rows), t]
+    assert rest.min() < 1e-3 and rest.max() > 0.3 and abs(wlse).min() > 60
+    # logits: d + 8 steps of L, of the target and of the others, as far as they matter; the maximum's product and the sum of eight terms of at most
+    # one, its logarithm and the products that follow: 32 steps of one, and of the loss
+    within(loss, want, F * (rest * 2 * (d + 8) * L + 32 * (1 + want)), "loss")
+    # what is handed to the gradients: one rounding of lse besides
+    within(lse, wlse, F * ((d + 8) * L + 32 * (1 + want) + abs(wlse)), "lse")
