@@ -7,7 +7,7 @@
 // are folded in ascending order; dW holds items and streams rows.  The other items' p and e are rounded to the storage type, as operands
 // of the last products (half a step each, of terms that are summed in fp32); the target's e = p - 1, which may be small beside p, is formed in
 // fp32 once a row, from the stored lse (whose own rounding is what is left of its error): for dX it stays out of the product and is added at the fold.
-// Bound by the matrix units: 8192 rows over 131072 items, d = 256, bf16: forward 500 us, 1.1 PFLOP/s, both gradients 1840 us with the
+// Bound by the matrix units: 8192 rows over 131072 items, d = 256, bf16: forward 500 us, 1.1 PFLOP/s, both gradients 1830 us with the
 // logits' products done again on either side, 1.2 PFLOP/s, where a library product of 16384^3 reaches 1.36.  (Logits kept for the
 // gradients would be 2 GB written and read twice, as long as the product that they save.)
 #include <algorithm>

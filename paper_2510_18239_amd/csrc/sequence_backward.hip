@@ -16,7 +16,7 @@
 // Bound by the two units waiting for each other: matrix cores busy 45 and 38 % of the time in the two kernels, the vector units about half
 // (of the second, at d/h = 64: 512 cycles of products and some 620 of exponentials, products and rounding a block of 32 queries, which takes
 // 1350; two waves a SIMD are not enough to cover for each other).  16 causal histories of 4096 events, four heads on two, d/h = 64
-// 560 us, 980 TFLOP/s of the eight products, 615 of the five; d/h = 128 1170 us, 940 and 590.
+// 550 us, 1 PFLOP/s of the eight products, 625 TFLOP/s of the five; d/h = 128 1160 us, 945 and 590.
 #include <algorithm>
 
 #include "fold.hpp"
